@@ -363,6 +363,178 @@ dex_status dex_debug_gumbel(uint64_t seed, int32_t seq, int32_t pos, int32_t V, 
  * traffic counters against a kernel of known size.                          */
 dex_status dex_debug_copy(void *dst, const void *src, int64_t bytes, void *hip_stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators over a paged key/value cache, for programs that bring their own
+ * layers: rotary positions and the cache write, attention of one new token,
+ * page tables that fork, grow and compact, and beam selection.
+ *
+ *   - The cache is the caller's device memory: keys and values of a layer are
+ *     [n_pages][n_kv_heads][page_size][head_dim] each (16-byte aligned), a
+ *     pool of layers [n_layers] of those.  page_size is a power of two, 1 to
+ *     1024.  Position p of sequence s is slot p % page_size of page
+ *     table[s][p / page_size] (device int32 [n_seqs][max_pages]); an entry
+ *     outside [0, n_pages), -1 by custom, is no page.  n_pages * n_kv_heads *
+ *     page_size < 2^32 - 1, n_pages <= 2^30.
+ *   - All arrays are device memory unless they are called host arrays; all
+ *     work is enqueued on hip_stream, which belongs to the current device, and
+ *     nothing is allocated, copied to the host or waited for, so every call
+ *     can be captured into a graph.  What a call reads on the device (lengths,
+ *     tables, parents) may change between replays; its sizes may not.
+ *   - Work memory is the caller's: the size that the matching _work function
+ *     gives, 16-byte aligned, with any contents.  It is free for another use
+ *     once the call's work is done; two calls that may overlap in time (two
+ *     streams, two graphs) need one each.
+ *   - Argument errors return DEX_E_INVAL before anything is launched, with
+ *     the reason in dex_last_error(NULL).  Numbers on the device cannot be
+ *     refused; each call says what it makes of those that do not fit, and
+ *     none reads or writes outside its arrays for them.
+ * ------------------------------------------------------------------------- */
+
+/* Rotary positions: pair i of a head, i < rot_dim / 2, turns by position *
+ * f_i, f_i = theta^(-2 i / rot_dim), and is scaled by `amplitude`; dimensions
+ * from rot_dim on stay as they are.  Pairs are (i, i + rot_dim / 2), or
+ * (2 i, 2 i + 1) where interleaved.  `turns` holds f_i / 2 pi in double.     */
+typedef struct {
+  const double *turns;                  /* device [rot_dim / 2] */
+  int32_t rot_dim;                      /* even, 2 .. head_dim */
+  int32_t interleaved;
+  float amplitude;
+} dex_rotary;
+
+enum {
+  DEX_ROTARY_PLAIN = 0,
+  DEX_ROTARY_LINEAR = 1,                /* f_i / factor (positions interpolated) */
+  DEX_ROTARY_BASE = 2,                  /* theta * factor^(rot_dim / (rot_dim - 2)) */
+  DEX_ROTARY_BANDS = 3                  /* f_i where it makes at least `fast` turns over the
+                                           original context, f_i / factor where at most
+                                           `slow`, in proportion between */
+};
+
+/* The plan's turns (HOST double [rot_dim / 2]).  factor is read by every
+ * scaling but PLAIN; original, slow and fast (0 <= slow < fast) by BANDS.    */
+dex_status dex_rotary_turns(int32_t scaling, int32_t rot_dim, double theta, double factor, double original,
+                            double slow, double fast, double *turns);
+
+/* Turns queries and keys, or one of them (n_heads or n_kv_heads 0 and null
+ * arrays): q_out[r][h] = R(pos[r]) q[r][h].  Element d of head h of row r lies
+ * at row * row_stride + h * head_stride + d of its array, strides in elements
+ * of dtype.  An output may be its input with the same strides, or memory that
+ * overlaps no input.  inverse: turns back, R(-pos), which is also the
+ * rotation's gradient.  Positions are any int32; the angle is formed in
+ * double.  n_rows * head_dim * (n_heads + n_kv_heads + 8) < 2^35.            */
+dex_status dex_rope(int32_t dtype, int32_t head_dim, const dex_rotary *rotary, int32_t inverse, int32_t n_rows,
+                    const int32_t *pos, const void *q, int64_t q_row, int64_t q_head, int32_t n_heads, void *q_out,
+                    int64_t q_out_row, int64_t q_out_head, const void *k, int64_t k_row, int64_t k_head,
+                    int32_t n_kv_heads, void *k_out, int64_t k_out_row, int64_t k_out_head, void *hip_stream);
+
+/* The cache write of one layer, with the rotation: row r's keys, turned, and
+ * its values go to position row_pos[r] of sequence row_seq[r] (NULL: r), its
+ * queries, turned, to q_out (n_heads 0 and null arrays: no queries).  rotary
+ * NULL: nothing turns.  A row whose position is negative, whose sequence is
+ * not in [0, n_seqs) or whose page is not there is left out altogether.  Rows
+ * must not share a position of a sequence, nor sequences a page written to
+ * (dex_pages_reserve sees to that).  Limits as dex_rope's, with the values'
+ * heads.                                                                    */
+dex_status dex_pages_append(int32_t dtype, int32_t head_dim, const dex_rotary *rotary, int32_t n_rows,
+                            const int32_t *row_seq, const int32_t *row_pos, const void *q, int64_t q_row,
+                            int64_t q_head, int32_t n_heads, void *q_out, int64_t q_out_row, int64_t q_out_head,
+                            const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                            int64_t v_head, int32_t n_kv_heads, void *k_pages, void *v_pages, int32_t n_pages,
+                            int32_t page_size, const int32_t *table, int32_t n_seqs, int32_t max_pages,
+                            void *hip_stream);
+
+/* Attention of one new token a row over one layer: row r (sequence
+ * row_seq[r], NULL: r) with query head h attends to the keys j < row_len[r]
+ * of kv head h / (n_heads / n_kv_heads), with a window only to the last
+ * `window` of them (0: all), and only where the page is there:
+ *   s_j = scale q.k_j,  out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m),
+ *   lse = m + ln sum_j e^(s_j - m)   (float [n_rows][n_heads], or NULL).
+ * A row that sees no key (row_len <= 0, a sequence outside [0, n_seqs), no
+ * page) gets zeros and -inf.  No row_len exceeds max_len, which sizes the
+ * work: keys past it, or past the table, are not attended to.  head_dim 32,
+ * 64 or 128; n_heads a multiple of n_kv_heads, at most 64 times it; q, out and
+ * the cache are of dtype, sums and statistics float.  Consecutive `group` rows
+ * whose leading pages are the same (the beams of a request) have those read
+ * once for all of them; any group gives the same bits.  A row's bits depend on
+ * its own keys and query alone.                                             */
+int64_t dex_pages_attention_work(int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                 int32_t max_len);
+dex_status dex_pages_attention(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads, int32_t n_rows,
+                               const int32_t *row_seq, const int32_t *row_len, int32_t max_len, int32_t window,
+                               int32_t group, float scale, const void *q, int64_t q_row, int64_t q_head,
+                               const void *k_pages, const void *v_pages, int32_t n_pages, int32_t page_size,
+                               const int32_t *table, int32_t n_seqs, int32_t max_pages, void *out, int64_t out_row,
+                               int64_t out_head, float *lse, void *work, void *hip_stream);
+
+/* Page tables.  ref[p] (int32 [n_pages]) counts the holders of page p: the
+ * table rows that list it and any others the caller counts (a cached prefix);
+ * 0 is free.  length[s] is the sequence's tokens.  Table entries behind a
+ * sequence's pages are -1.  n_seqs <= 1024 here.
+ *
+ * dex_pages_fork: sequence s becomes a copy of sequence parent[s], sharing its
+ * pages, or empty where parent[s] is not in [0, n_seqs).  Sequences that are
+ * nobody's parent lose their pages, which are free once ref is 0; so a call
+ * with parent[s] = s for some and -1 for others frees the others.  Each output
+ * may be its input.                                                         */
+dex_status dex_pages_fork(const int32_t *table, const int32_t *ref, const int32_t *length, const int32_t *parent,
+                          int32_t n_seqs, int32_t max_pages, int32_t n_pages, int32_t *table_out, int32_t *ref_out,
+                          int32_t *length_out, void *hip_stream);
+
+/* Room for n_new[s] >= 0 more tokens (below 0 counts as 0) of every sequence,
+ * which may then write positions length[s] .. length[s] + n_new[s] - 1.  Pages
+ * are taken lowest number first, for the sequences in order.  A partly filled
+ * last page that others hold too is replaced by one of the sequence's own, and
+ * (src, dst, tokens) says what dex_pages_copy has to copy before the next
+ * write: its first `tokens` slots.  The last of several writers keeps the page
+ * if no one else holds it.  Writes
+ *   table, ref, length   updated (length[s] += n_new[s]);
+ *   pos[s]     the first new position, or -1 (nothing asked, or not granted);
+ *   src, dst, tokens     int32 [n_seqs], the copies first, then -1, -1, 0;
+ *   state      int32 [4]: copies, pages taken, pages missing, 1 if a sequence
+ *              outgrows the table or has a length below 0.
+ * Unless state[2] and state[3] are 0 nothing was granted: table, ref and length
+ * stay, every pos is -1 and the list is empty.                              */
+dex_status dex_pages_reserve(int32_t *table, int32_t *ref, int32_t *length, const int32_t *n_new, int32_t n_seqs,
+                             int32_t max_pages, int32_t n_pages, int32_t page_size, int32_t *pos, int32_t *src,
+                             int32_t *dst, int32_t *tokens, int32_t *state, void *hip_stream);
+
+/* Moves the n pages in use (ref > 0) to pages 0 .. n - 1: the i-th of those at
+ * or past n goes to the i-th free page before it.  map[p] (int32 [n_pages]) is
+ * page p's new number, -1 for a free page; src and dst (int32 [n_pages / 2])
+ * list the moves for dex_pages_copy, then -1; state as above: moves, n, 0, 0.
+ * table_out and ref_out may be their inputs.                                */
+dex_status dex_pages_compact(const int32_t *table, const int32_t *ref, int32_t n_seqs, int32_t max_pages,
+                             int32_t n_pages, int32_t *table_out, int32_t *ref_out, int32_t *map, int32_t *src,
+                             int32_t *dst, int32_t *state, void *hip_stream);
+
+/* Copies pages of every layer of a pool: entry i, i < min(*count, capacity)
+ * (count NULL: capacity), copies the first tokens[i] slots (NULL: all) of page
+ * src[i] to page dst[i], keys and values.  An entry with a page outside
+ * [0, n_pages) copies nothing.  No page may be a dst twice, or both src and
+ * dst.  A head's row of head_dim elements is a multiple of 16 bytes.         */
+dex_status dex_pages_copy(int32_t dtype, int32_t head_dim, int32_t n_layers, int32_t n_pages, int32_t n_kv_heads,
+                          int32_t page_size, void *k_pool, void *v_pool, const int32_t *src, const int32_t *dst,
+                          const int32_t *tokens, const int32_t *count, int32_t capacity, void *hip_stream);
+
+/* Beam search's selection.  Candidate (beam, token) of a request has total
+ * score[beam] + logit - lse(the beam's logits); a finished beam (done, uint8
+ * or NULL) has one candidate, (beam, eos) with its score as it is, the others
+ * -inf.  A score that is not finite, and logits with a NaN, a +inf or nothing
+ * but -inf, make all the beam's totals -inf.  Writes the n_out candidates of
+ * largest total, largest first, equal ones by beam and token: parent (row
+ * request * beams + beam, as dex_pages_fork takes it), token, score (the
+ * total), done (the beam's, or token == eos; NULL: not wanted).  Within a beam
+ * candidates are compared by their logits, across beams in double.  logits:
+ * [requests * beams][vocab] of dtype, rows ld elements apart, any alignment.
+ * beams and n_out 1 .. 64, n_out <= beams * vocab, requests * beams <= 2^20,
+ * requests * beams * vocab of at most 2^31 segments of 2048; eos in
+ * [0, vocab), or -1 (with done NULL): none.                                  */
+int64_t dex_beam_select_work(int32_t dtype, int32_t requests, int32_t beams, int32_t vocab, int32_t n_out);
+dex_status dex_beam_select(int32_t dtype, const void *logits, int64_t ld, int32_t requests, int32_t beams,
+                           int32_t vocab, const float *score, const uint8_t *done, int32_t eos, int32_t n_out,
+                           int32_t *parent, int32_t *token, float *score_out, uint8_t *done_out, void *work,
+                           void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

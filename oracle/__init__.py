@@ -9,9 +9,9 @@ teacher-forced exit logits), lattice (Algorithm 1 / Section 3.2 bookkeeping
 with Algorithm 2's masks), dex (the full procedure on the model), gumbel
 (Algorithm 2's sampling-mode noise and decode rule), adapter (the inducing
 adapter of non-final depths), ead (Section 2's accounting, used as test
-pins).
+pins), paged (the operators over a paged key/value cache).
 """
-from . import adapter, ar, dex, ead, gumbel, lattice, model  # noqa: F401
+from . import adapter, ar, dex, ead, gumbel, lattice, model, paged  # noqa: F401
 from .model import Model  # noqa: F401
 
 

@@ -32,6 +32,7 @@
 
 #include "dex.h"
 #include "dex_kernels.h"
+#include "paged.h"
 
 using namespace dex;
 
@@ -815,6 +816,12 @@ void stop_lane_workers(dex_ctx *ctx) {
 }
 
 }  // namespace
+
+namespace dex {
+void set_call_error(const char *msg) noexcept {
+  try { g_create_error = msg; } catch (...) { g_create_error.clear(); }
+}
+}  // namespace dex
 
 // ===================================================================== ABI
 extern "C" {

@@ -28,6 +28,9 @@ EXPORTED = (
     "dex_debug_kernel_times", "dex_debug_time_kernel", "dex_debug_gemm", "dex_debug_attention",
     "dex_debug_gumbel", "dex_debug_copy", "dex_debug_plan", "dex_debug_attention_noalloc",
     "dex_debug_set_round_timing", "dex_debug_round_times",
+    "dex_rotary_turns", "dex_rope", "dex_pages_append", "dex_pages_attention", "dex_pages_attention_work",
+    "dex_pages_fork", "dex_pages_reserve", "dex_pages_compact", "dex_pages_copy", "dex_beam_select",
+    "dex_beam_select_work",
 )
 
 
@@ -72,6 +75,11 @@ class DexStepInfo(ctypes.Structure):
     ]
 
 
+class DexRotary(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("amplitude", ctypes.c_float)]
+
+
 _lib = None
 
 
@@ -110,8 +118,25 @@ def load(path: str | None = None):
     lib.dex_debug_set_round_timing.argtypes = [vp, i32]
     lib.dex_debug_round_times.argtypes = [vp, i32, P(ctypes.c_double), P(i64)]
     lib.dex_debug_plan.argtypes = [i32, i32, i32, i32, P(i32), i32, P(i32), i32, P(i32)]
+    f32, f64 = ctypes.c_float, ctypes.c_double
+    heads = [vp, i64, i64]                           # an array of heads: data, row and head strides
+    lib.dex_rotary_turns.argtypes = [i32, i32, f64, f64, f64, f64, f64, P(f64)]
+    lib.dex_rope.argtypes = [i32, i32, P(DexRotary), i32, i32, vp, *heads, i32, *heads, *heads, i32, *heads, vp]
+    lib.dex_pages_append.argtypes = [i32, i32, P(DexRotary), i32, vp, vp, *heads, i32, *heads, *heads, *heads, i32,
+                                     vp, vp, i32, i32, vp, i32, i32, vp]
+    lib.dex_pages_attention_work.argtypes = [i32] * 5
+    lib.dex_pages_attention.argtypes = [i32, i32, i32, i32, i32, vp, vp, i32, i32, i32, f32, *heads, vp, vp, i32, i32,
+                                        vp, i32, i32, *heads, vp, vp, vp]
+    lib.dex_pages_fork.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]
+    lib.dex_pages_reserve.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.dex_pages_compact.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.dex_pages_copy.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp]
+    lib.dex_beam_select_work.argtypes = [i32] * 5
+    lib.dex_beam_select.argtypes = [i32, vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
     for name in EXPORTED:
-        if name not in ("dex_destroy", "dex_last_error"):
+        if name.endswith("_work"):
+            getattr(lib, name).restype = i64
+        elif name not in ("dex_destroy", "dex_last_error"):
             getattr(lib, name).restype = ctypes.c_int32
     if path is None:
         _lib = lib

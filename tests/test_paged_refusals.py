@@ -1,0 +1,163 @@
+"""The paged-cache entry points refuse bad arguments on the host, before any
+device call, with the reason in dex_last_error(NULL); the binding refuses
+tensors that do not fit.  (The valid base arguments are never passed
+unchanged: their addresses are no memory.)"""
+import ctypes
+import math
+import os
+
+import numpy as np
+import pytest
+
+from oracle import paged as ref
+from paper_2606_29223_amd import dexlib, paged
+
+FAKE = 0x1000
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(dexlib.LIB_PATH):
+        pytest.skip("libdex.so not built")
+    return dexlib.load()
+
+
+PLAN = dict(turns=FAKE, rot_dim=64, interleaved=0, amplitude=1.0)
+ROPE = dict(dtype=1, head_dim=64, plan=PLAN, inverse=0, n_rows=2, pos=FAKE, q=FAKE, q_row=256, q_head=64, n_heads=4,
+            q_out=FAKE, qo_row=256, qo_head=64, k=FAKE, k_row=128, k_head=64, n_kv=2, k_out=FAKE, ko_row=128, ko_head=64)
+APPEND = dict(dtype=1, head_dim=64, plan=PLAN, n_rows=2, seq=None, pos=FAKE, q=FAKE, q_row=256, q_head=64, n_heads=4,
+              q_out=FAKE, qo_row=256, qo_head=64, k=FAKE, k_row=128, k_head=64, v=FAKE, v_row=128, v_head=64, n_kv=2,
+              k_pages=FAKE, v_pages=FAKE, n_pages=8, page_size=16, table=FAKE, n_seqs=2, max_pages=4)
+ATTENTION = dict(dtype=1, head_dim=64, n_heads=4, n_kv=2, n_rows=2, seq=None, lens=FAKE, max_len=600, window=0, group=1,
+                 scale=0.125, q=FAKE, q_row=256, q_head=64, k_pages=FAKE, v_pages=FAKE, n_pages=80, page_size=16,
+                 table=FAKE, n_seqs=2, max_pages=40, out=FAKE, o_row=256, o_head=64, lse=None, work=FAKE)
+FORK = dict(table=FAKE, ref=FAKE, length=FAKE, parent=FAKE, n_seqs=2, max_pages=4, n_pages=8, t=FAKE, r=FAKE, n=FAKE)
+RESERVE = dict(table=FAKE, ref=FAKE, length=FAKE, n_new=FAKE, n_seqs=2, max_pages=4, n_pages=8, page_size=16, pos=FAKE,
+               src=FAKE, dst=FAKE, tokens=FAKE, state=FAKE)
+COMPACT = dict(table=FAKE, ref=FAKE, n_seqs=2, max_pages=4, n_pages=8, t=FAKE, r=FAKE, map=FAKE, src=FAKE, dst=FAKE,
+               state=FAKE)
+COPY = dict(dtype=1, head_dim=64, n_layers=2, n_pages=8, n_kv=2, page_size=16, k=FAKE, v=FAKE, src=FAKE, dst=FAKE,
+            tokens=None, count=None, capacity=3)
+BEAM = dict(dtype=1, logits=FAKE, ld=500, requests=2, beams=4, vocab=500, score=FAKE, done=None, eos=-1, n_out=4,
+            parent=FAKE, token=FAKE, score_out=FAKE, done_out=None, work=FAKE)
+
+
+def _call(lib, name, base, **kw):
+    args = dict(base, **kw)
+    if "plan" in args:
+        p = args["plan"]
+        args["plan"] = None if p is None else ctypes.byref(dexlib.DexRotary(**p))
+    return getattr(lib, name)(*args.values(), None)
+
+
+CACHE = [(dict(dtype=2), "dtype"), (dict(head_dim=63), "head_dim"), (dict(head_dim=0), "head_dim"),
+         (dict(page_size=24), "power of two"), (dict(page_size=0), "power of two"), (dict(page_size=2048), "power of two"),
+         (dict(n_pages=0), "n_pages"), (dict(n_pages=1 << 30, page_size=16), "2^32"), (dict(n_kv=0), "n_kv_heads")]
+TABLE = [(dict(n_seqs=0), "n_seqs"), (dict(max_pages=0), "max_pages"), (dict(max_pages=1 << 28), "position")]
+ROTARY = [(dict(plan=dict(PLAN, turns=None)), "turns"), (dict(plan=dict(PLAN, rot_dim=66)), "rot_dim"),
+          (dict(plan=dict(PLAN, rot_dim=7)), "rot_dim"), (dict(plan=dict(PLAN, rot_dim=0)), "rot_dim"),
+          (dict(plan=dict(PLAN, amplitude=math.nan)), "amplitude")]
+QUERIES = [(dict(q=None), "queries"), (dict(n_heads=0), "queries"), (dict(n_heads=-1), "queries"), (dict(q_out=None), "")]
+BAD = (
+    [("dex_rope", ROPE, *b) for b in ROTARY + QUERIES + [
+        (dict(plan=None), "rotary"), (dict(dtype=3), "dtype"), (dict(head_dim=62), "rot_dim"), (dict(k=None), "keys"),
+        (dict(k_out=None), "output"), (dict(pos=None), "pos"), (dict(n_rows=-1), "n_rows"),
+        (dict(q=None, n_heads=0, k=None, n_kv=0), "neither"), (dict(n_rows=1 << 26), "too many")]]
+    + [("dex_pages_append", APPEND, *b) for b in CACHE + TABLE + ROTARY + QUERIES + [
+        (dict(k=None), "NULL"), (dict(v=None), "NULL"), (dict(k_pages=None), "NULL"), (dict(v_pages=None), "NULL"),
+        (dict(table=None), "NULL"), (dict(k_pages=FAKE + 8), "aligned"), (dict(v_pages=FAKE + 2), "aligned"),
+        (dict(pos=None), "row_pos"), (dict(n_rows=-5), "n_rows"), (dict(n_rows=1 << 26), "too many")]]
+    + [("dex_pages_attention", ATTENTION, *b) for b in CACHE + TABLE + [
+        (dict(head_dim=96), "head_dim"), (dict(n_heads=3), "multiple"), (dict(n_heads=1), "multiple"),
+        (dict(n_heads=130), "64 times"), (dict(n_rows=-1), "n_rows"), (dict(max_len=-1), "max_len"),
+        (dict(window=-1), "window"), (dict(group=0), "group"), (dict(scale=math.inf), "scale"), (dict(q=None), "NULL"),
+        (dict(lens=None), "NULL"), (dict(out=None), "NULL"), (dict(table=None), "NULL"), (dict(work=None), "work"),
+        (dict(work=FAKE + 4), "work"), (dict(k_pages=FAKE + 4), "aligned")]]
+    + [("dex_pages_fork", FORK, *b) for b in TABLE + [
+        (dict(n_seqs=1025), "n_seqs"), (dict(n_pages=0), "n_pages"), (dict(parent=None), "NULL"), (dict(t=None), "NULL"),
+        (dict(max_pages=-3), "max_pages")] if b[0] != dict(max_pages=1 << 28)]
+    + [("dex_pages_reserve", RESERVE, *b) for b in TABLE + [
+        (dict(n_seqs=1025), "n_seqs"), (dict(n_pages=(1 << 30) + 1), "n_pages"), (dict(page_size=3), "power of two"),
+        (dict(n_new=None), "NULL"), (dict(state=None), "NULL"), (dict(tokens=None), "NULL")]]
+    + [("dex_pages_compact", COMPACT, *b) for b in [
+        (dict(n_pages=0), "n_pages"), (dict(src=None), "NULL"), (dict(map=None), "NULL"), (dict(n_seqs=0), "n_seqs"),
+        (dict(max_pages=0), "max_pages")]]
+    + [("dex_pages_copy", COPY, *b) for b in CACHE + [
+        (dict(head_dim=4), "16 bytes"), (dict(n_layers=0), "n_layers"), (dict(capacity=-1), "capacity"),
+        (dict(k=None), "NULL"), (dict(src=None), "NULL"), (dict(v=FAKE + 8), "aligned")]]
+    + [("dex_beam_select", BEAM, *b) for b in [
+        (dict(dtype=-1), "dtype"), (dict(beams=0), "beams"), (dict(beams=65), "beams"), (dict(n_out=0), "n_out"),
+        (dict(n_out=65), "n_out"), (dict(vocab=0), "vocab"), (dict(vocab=1, n_out=5), "n_out"), (dict(eos=500), "eos"),
+        (dict(eos=-2), "eos"), (dict(done=FAKE), "eos"), (dict(ld=499), "ld"), (dict(requests=-1), "requests"),
+        (dict(requests=1 << 19), "2^20"), (dict(requests=1 << 18, beams=4, vocab=1 << 26, ld=1 << 26), "too many"),
+        (dict(score=None), "NULL"), (dict(work=None), "NULL"), (dict(work=FAKE + 8), "aligned"),
+        (dict(logits=FAKE + 1), "aligned")]]
+)
+
+
+@pytest.mark.parametrize("i", range(len(BAD)))
+def test_bad_arguments_are_refused(lib, i):
+    name, base, change, why = BAD[i]
+    assert _call(lib, name, base, **change) == dexlib.DEX_E_INVAL, (name, change)
+    msg = lib.dex_last_error(None).decode()
+    assert msg.startswith(name + ": ") and why in msg, (msg, change)
+
+
+def test_no_rows_is_no_work(lib):
+    assert _call(lib, "dex_rope", ROPE, n_rows=0) == dexlib.DEX_OK
+    assert _call(lib, "dex_pages_append", APPEND, n_rows=0) == dexlib.DEX_OK
+    assert _call(lib, "dex_pages_attention", ATTENTION, n_rows=0) == dexlib.DEX_OK
+    assert _call(lib, "dex_pages_copy", COPY, capacity=0) == dexlib.DEX_OK
+    assert _call(lib, "dex_beam_select", BEAM, requests=0) == dexlib.DEX_OK
+
+
+def test_work_sizes(lib):
+    assert lib.dex_pages_attention_work(4, 32, 8, 128, 100) >= 0
+    small, big = (lib.dex_pages_attention_work(4, 32, 8, 128, n) for n in (4096, 65536))
+    assert 0 < small < big
+    assert lib.dex_pages_attention_work(1 << 20, 32, 8, 128, 1 << 20) < 1 << 40      # rows go 1024 at a time
+    assert lib.dex_beam_select_work(1, 2, 4, 500, 4) > 0
+    assert lib.dex_beam_select_work(7, 2, 4, 500, 4) == 0
+
+
+SCALINGS = [dict(scaling=None), dict(scaling="linear", factor=4.0), dict(scaling="base", factor=8.0),
+            dict(scaling="bands", factor=16.0, original=8192.0, slow=1.0, fast=32.0)]
+
+
+@pytest.mark.parametrize("kw", SCALINGS, ids=lambda k: str(k["scaling"]))
+@pytest.mark.parametrize("rot", [4, 64, 128])
+def test_turns_are_the_frequencies(lib, kw, rot):
+    got = (ctypes.c_double * (rot // 2))()
+    args = dict(dict(factor=1.0, original=0.0, slow=1.0, fast=32.0), **kw)
+    st = lib.dex_rotary_turns(paged.SCALING[args["scaling"]], rot, 5e5, args["factor"], args["original"], args["slow"],
+                              args["fast"], got)
+    assert st == dexlib.DEX_OK
+    # a few roundings of 2^-53 in each of power, division and band
+    np.testing.assert_allclose(np.array(got) * 2 * math.pi, ref.frequencies(rot, 5e5, **kw), rtol=1e-14)
+
+
+@pytest.mark.parametrize("args", [(4, 64, 1e4, 1, 1, 1, 2), (-1, 64, 1e4, 1, 1, 1, 2), (0, 63, 1e4, 1, 1, 1, 2),
+                                  (0, 0, 1e4, 1, 1, 1, 2), (0, 64, 0.0, 1, 1, 1, 2), (0, 64, math.nan, 1, 1, 1, 2),
+                                  (1, 64, 1e4, 0.0, 1, 1, 2), (1, 64, 1e4, math.inf, 1, 1, 2), (2, 2, 1e4, 4, 1, 1, 2),
+                                  (3, 64, 1e4, 4, 0.0, 1, 2), (3, 64, 1e4, 4, 4096, 2, 2), (3, 64, 1e4, 4, 4096, -1, 2)])
+def test_bad_plans_are_refused(lib, args):
+    assert lib.dex_rotary_turns(*args, (ctypes.c_double * 64)()) == dexlib.DEX_E_INVAL
+    assert lib.dex_last_error(None).decode().startswith("dex_rotary_turns: ")
+
+
+def test_the_binding_refuses_tensors_off_the_gpu(lib):
+    torch = pytest.importorskip("torch")
+    plan = paged.Rotary(8, device="cpu")
+    x, n = torch.zeros(2, 3, 8), torch.zeros(2, dtype=torch.int32)
+    pages = torch.zeros(4, 3, 4, 8)
+    table, ref_ = torch.zeros((2, 2), dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: paged.rope(plan, n, x), lambda: paged.append(pages, pages, table, n, x, x),
+                 lambda: paged.attention(x, pages, pages, table, n), lambda: paged.fork(table, ref_, n, n),
+                 lambda: paged.reserve(table, ref_, n, n, 4), lambda: paged.compact(table, ref_),
+                 lambda: paged.copy(pages[None], pages[None], n, n),
+                 lambda: paged.beam_select(torch.zeros(4, 9), torch.zeros(2, 2)),
+                 lambda: paged.Rotary(8, scaling="cubic"), lambda: paged.Rotary(8, rot_dim=10),
+                 lambda: paged.Rotary(8, rot_dim=3), lambda: paged.Rotary(8, scaling="linear", factor=0)):
+        with pytest.raises(dexlib.DexError) as e:
+            call()
+        assert e.value.status == dexlib.DEX_E_INVAL
