@@ -381,7 +381,7 @@ dex_status dex_debug_copy(void *dst, const void *src, int64_t bytes, void *hip_s
  *     can be captured into a graph.  What a call reads on the device (lengths,
  *     tables, parents) may change between replays; its sizes may not.
  *   - Work memory is the caller's: the size that the matching _work function
- *     gives, 16-byte aligned, with any contents.  It is free for another use
+ *     gives (0: may be NULL), 16-byte aligned, with any contents.  It is free for another use
  *     once the call's work is done; two calls that may overlap in time (two
  *     streams, two graphs) need one each.
  *   - Argument errors return DEX_E_INVAL before anything is launched, with
@@ -458,7 +458,7 @@ dex_status dex_pages_append(int32_t dtype, int32_t head_dim, const dex_rotary *r
  * once for all of them; any group gives the same bits.  A row's bits depend on
  * its own keys and query alone.                                             */
 int64_t dex_pages_attention_work(int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
-                                 int32_t max_len);
+                                 int32_t max_len, int32_t group);
 dex_status dex_pages_attention(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads, int32_t n_rows,
                                const int32_t *row_seq, const int32_t *row_len, int32_t max_len, int32_t window,
                                int32_t group, float scale, const void *q, int64_t q_row, int64_t q_head,

@@ -165,9 +165,10 @@ dex_status dex_pages_append(int32_t dtype, int32_t head_dim, const dex_rotary *r
   return launched(fn, launch_rope(dtype, a, (hipStream_t)stream));
 }
 
-int64_t dex_pages_attention_work(int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_len) {
-  if (n_rows < 0 || n_heads < 1 || n_kv_heads < 1 || head_dim < 1 || max_len < 0) return 0;
-  return (int64_t)paged_attention_work(n_rows, n_heads, head_dim, max_len);
+int64_t dex_pages_attention_work(int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_len,
+                                 int32_t group) {
+  if (n_rows < 0 || n_heads < 1 || n_kv_heads < 1 || head_dim < 1 || max_len < 0 || group < 1) return 0;
+  return (int64_t)paged_attention_work(n_rows, n_heads, head_dim, max_len, group);
 }
 
 dex_status dex_pages_attention(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads, int32_t n_rows,
@@ -194,7 +195,7 @@ dex_status dex_pages_attention(int32_t dtype, int32_t head_dim, int32_t n_heads,
   a.seq = row_seq; a.len = row_len; a.n_rows = n_rows; a.n_heads = n_heads; a.head_dim = head_dim;
   a.group = group; a.max_len = max_len; a.window = window; a.scale = scale;
   a.out = out; a.out_row = out_row; a.out_head = out_head; a.lse = lse; a.work = work;
-  REFUSE_IF(paged_attention_work(n_rows, n_heads, head_dim, max_len) > 0 && (!work || !aligned(work, 16)),
+  REFUSE_IF(paged_attention_work(n_rows, n_heads, head_dim, max_len, group) > 0 && (!work || !aligned(work, 16)),
             "the work memory is NULL or not 16-byte aligned");
   return launched(fn, launch_paged_attention(dtype, a, (hipStream_t)stream));
 }

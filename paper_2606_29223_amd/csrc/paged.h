@@ -108,7 +108,7 @@ struct PagedAttnArgs {
   float *lse;                 // [n_rows][n_heads], or null
   void *work;                 // paged_attention_work bytes
 };
-size_t paged_attention_work(int n_rows, int n_heads, int head_dim, int max_len);
+size_t paged_attention_work(int n_rows, int n_heads, int head_dim, int max_len, int group);
 hipError_t launch_paged_attention(int dtype, const PagedAttnArgs &a, hipStream_t s);
 
 constexpr int kMaxBeams = 64;

@@ -3,23 +3,26 @@
 //
 // Row r with query heads h sees the keys lo <= j < len of its sequence whose
 // page is there: s_j = scale q.k_j, out = sum e^{s_j - m} v_j / sum e^{s_j - m},
-// lse = m + ln sum e^{s_j - m}.  A split is 256 keys at a fixed place of the
-// sequence; its record (sum of v, m, sum) goes to the join, which adds a
-// row's records in order, so a row's bits depend on its own keys alone.
+// lse = m + ln sum e^{s_j - m}.
 //
-// A workgroup takes (row, kv head, split) items, 64 keys (32 in fp32) of a
-// split a wave:  S^T = K Q^T and O^T = V^T P^T on the matrix cores, the kv
-// head's query heads as the 16 columns, so each lane holds the scores and
-// outputs of one query head.  The kernel reads each key and value once from
-// HBM and is bound by that: the products are 4 % of what the matrix cores
-// could do meanwhile, which is why P goes through them in two bf16 parts
-// (p = hi + lo to 2^-17) and costs the output no accuracy.
+// A row's keys are cut into units of 64 at fixed places of the sequence, its
+// units into at most 96 runs of 2^n units, and four runs are a split (RowPlan).
+// A workgroup takes a split, a wave each run with a running maximum and sum;
+// the four meet in LDS, and the join adds a row's splits in a fixed order.  All
+// of that follows from the row's own length and window, so its bits do not
+// depend on the call's other rows.
+//
+// A unit is S^T = K Q^T and O^T = V^T P^T on the matrix cores, the kv head's
+// query heads as columns, so that each lane holds the scores and outputs of
+// one query head.  Keys and values are read once from HBM, which bounds the
+// kernel; the products are 4 % of what the matrix cores could do meanwhile.
+// That is why P goes through them in two bf16 parts (p = hi + lo to 2^-17): it
+// costs the output no accuracy and no time.
 #include "attn_decode.h"
 #include "dex.h"
 #include "paged.h"
 
 #include <algorithm>
-#include <climits>
 
 namespace dex {
 
@@ -27,38 +30,41 @@ namespace {
 
 constexpr int PA_WAVES = 4;
 constexpr int PA_THREADS = PA_WAVES * 64;
-constexpr int PA_SPLIT = 256;             // keys of a split
-constexpr int PA_ROWS = 1024;             // rows of a launch
+constexpr int PA_UNIT = 64;               // keys of a unit
+constexpr int PA_SPLITS = 24;             // splits of a row at most
+constexpr int PA_ROWS = 512;              // rows of a launch
+constexpr int PA_COLS = 32;               // query heads of an item
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-// Splits of a row, and the first of them.
-__device__ __forceinline__ int row_splits(int len, int window, int *first) {
-  const int lo = window > 0 ? max(0, len - window) : 0;
-  *first = lo / PA_SPLIT;
-  return len > 0 ? (len - 1) / PA_SPLIT - *first + 1 : 1;      // an empty row has one item, to say so
+// How a row of `len` keys is cut: units [unit0, unit0 + units), 2^shift a run.
+struct RowPlan {
+  int lo, unit0, units, shift, n;         // lo: first key; n: splits
+};
+__host__ __device__ __forceinline__ RowPlan row_plan(int len, int window) {
+  RowPlan p;
+  p.lo = window > 0 && len > window ? len - window : 0;
+  p.unit0 = p.lo / PA_UNIT;
+  p.units = len > 0 ? (len - 1) / PA_UNIT - p.unit0 + 1 : 0;
+  p.shift = 0;
+  while ((p.units - 1) >> p.shift >= PA_SPLITS * PA_WAVES) ++p.shift;
+  p.n = len > 0 ? ((p.units - 1) >> p.shift) / PA_WAVES + 1 : 1;   // an empty row has one, to say so
+  return p;
 }
+constexpr int kSplitKeys = PA_UNIT * PA_WAVES;              // keys of a split, times 2^shift
 
-// What one wave makes of its keys of a split, for 16 NB columns: column r16
-// of block nb is query head nb * 16 + r16 of the kv head.
-template <int HD, int NB>
-struct WaveState {
-  float m[NB], l[NB];                     // in powers of two; m of the reference, l the lane's own keys' sum
-  pf_f32x4 o[NB][HD / 16];
-};
-
+// A wave's: the values (or keys) of a unit, then its part of a split's sums.
 template <typename T, int HD>
-struct Lds;
-template <int HD>
-struct Lds<uint16_t, HD> {                // V tile rows, then the wave's part of the sum
-  union {
-    uint16_t v[64][HD + 16];
-    float o[16][HD + 4];
-  };
-};
-template <int HD>
-struct Lds<float, HD> {
+union Lds {
+  uint16_t v[sizeof(T) == 2 ? PA_UNIT : 1][HD + 16];
   float o[16][HD + 4];
 };
+// Barrier for what the workgroup's waves leave each other in LDS; loads from
+// memory stay on their way across it.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 __device__ __forceinline__ float quad_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16, 64));
@@ -69,24 +75,25 @@ __device__ __forceinline__ float quad_sum(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
-// Scores of NT 16-key tiles to probabilities under the new reference; returns
-// by what the wave's earlier sums shrink.  Keys outside `mask` get 0.
+// Scores of NT 16-key tiles to powers of two under the new reference m; l is
+// this lane's part of their sum.  Keys outside `mask` get 0.  Returns by what
+// earlier sums shrink.
 template <int NT>
 __device__ __forceinline__ float soften(pf_f32x4 (&sc)[NT], unsigned long long mask, bool full, float scale2, float &m,
                                         float &l) {
-  const int grp = (threadIdx.x & 63) >> 4;
+  const unsigned long long mine = mask >> (4 * ((threadIdx.x & 63) >> 4));   // bit 16 nt + i: the lane's keys
   float mx = -INFINITY;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float v = sc[nt][i] * scale2;
-      if (!full && !(mask >> (nt * 16 + grp * 4 + i) & 1)) v = -INFINITY;
+      if (!full && !(mine >> (nt * 16 + i) & 1)) v = -INFINITY;
       sc[nt][i] = v;
       mx = fmaxf(mx, v);
     }
   const float m1 = fmaxf(m, quad_max(mx));
-  const float ref = m1 == -INFINITY ? 0.f : m1;       // nothing seen yet: every power is 0
+  const float ref = m1 == -INFINITY ? 0.f : m1;              // nothing seen yet: every power is 0
   const float shrink = __builtin_amdgcn_exp2f(m - ref);
   float sum = 0.f;
 #pragma unroll
@@ -96,181 +103,368 @@ __device__ __forceinline__ float soften(pf_f32x4 (&sc)[NT], unsigned long long m
       sc[nt][i] = __builtin_amdgcn_exp2f(sc[nt][i] - ref);
       sum += sc[nt][i];
     }
-  l = l * shrink + quad_sum(sum);
+  l = fmaf(l, shrink, sum);
   m = m1;
   return shrink;
 }
 
-// bf16: 64 keys at cache rows `mine` (lane j: key j; kNoRow: none).
-template <int HD, int NB>
-__device__ __forceinline__ void keys_bf16(const PagedAttnArgs &a, uint32_t mine, int nb_used,
-                                          const pf_bf16x8 (&qf)[NB][HD / 32], float scale2, Lds<uint16_t, HD> &lds,
-                                          WaveState<HD, NB> &w) {
-  constexpr int KS = HD / 32, DT = HD / 16, V4 = HD / 8, RPI = 64 / V4;
-  const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
-  const unsigned long long mask = __ballot(mine != kNoRow);
-  if (mask == 0) return;
-  const bool full = mask == ~0ull;
-  // an absent key reads row 0, which is there; its score and value are put out below
-  const uint32_t at = mine == kNoRow ? 0u : mine;
-  const uint16_t *kp = (const uint16_t *)a.k + grp * 8, *vp = (const uint16_t *)a.v + (lane % V4) * 8;
-  uint4 kf[4][KS], vv[V4];
-#pragma unroll
-  for (int nt = 0; nt < 4; ++nt) {
-    const uint16_t *row = kp + (size_t)(uint32_t)__shfl((int)at, nt * 16 + r16, 64) * HD;
-#pragma unroll
-    for (int st = 0; st < KS; ++st) kf[nt][st] = *(const uint4 *)(row + st * 32);
-  }
-#pragma unroll
-  for (int c = 0; c < V4; ++c)
-    vv[c] = *(const uint4 *)(vp + (size_t)(uint32_t)__shfl((int)at, c * RPI + lane / V4, 64) * HD);
-  pf_f32x4 sc[NB][4];
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    if (nb < nb_used) {
-#pragma unroll
-      for (int nt = 0; nt < 4; ++nt) {
-        sc[nb][nt] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int st = 0; st < KS; ++st)
-          sc[nb][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pf_bf16x8, kf[nt][st]), qf[nb][st],
-                                                               sc[nb][nt], 0, 0, 0);
-      }
-    }
-  }
-  if (!full) {
-#pragma unroll
-    for (int c = 0; c < V4; ++c)
-      if (!(mask >> (c * RPI + lane / V4) & 1)) vv[c] = make_uint4(0, 0, 0, 0);
-  }
-#pragma unroll
-  for (int c = 0; c < V4; ++c) *(uint4 *)&lds.v[c * RPI + lane / V4][(lane % V4) * 8] = vv[c];
-  wave_lds_sync();
-  const int tq = grp, ti = r16 >> 2, tg = lane & 3;
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    if (nb < nb_used) {
-      const float shrink = soften<4>(sc[nb], mask, full, scale2, w.m[nb], w.l[nb]);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) w.o[nb][dt] *= shrink;
-#pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        float p[8], r[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = sc[nb][2 * st + i / 4][i % 4];
-        const uint4 hi = make_uint4(pf_pack_bf16(p[0], p[1]), pf_pack_bf16(p[2], p[3]), pf_pack_bf16(p[4], p[5]),
-                                    pf_pack_bf16(p[6], p[7]));
-        const uint32_t hw[4] = {hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] = p[i] - __uint_as_float(i & 1 ? hw[i / 2] & 0xffff0000u : hw[i / 2] << 16);
-        const uint4 lo = make_uint4(pf_pack_bf16(r[0], r[1]), pf_pack_bf16(r[2], r[3]), pf_pack_bf16(r[4], r[5]),
-                                    pf_pack_bf16(r[6], r[7]));
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const pf_bf16x8 vf = tr_frag(&lds.v[32 * st + 4 * tq + ti][16 * dt + 4 * tg],
-                                       &lds.v[32 * st + 16 + 4 * tq + ti][16 * dt + 4 * tg]);
-          w.o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(pf_bf16x8, hi), w.o[nb][dt], 0, 0, 0);
-          w.o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(pf_bf16x8, lo), w.o[nb][dt], 0, 0, 0);
-        }
-      }
-    }
-  }
-  wave_lds_sync();                        // the tile is read before the next one is written
+// One wave's work on tiles of TK keys, for 16 NB columns (column r16 of block
+// nb).  `rows` of a tile: lane j holds the cache row of key j, or 0 where its
+// page is none (row 0 is there; what is read for a key that is not attended to
+// is put out).  Pages of 16 keys or more hold 16 neighbours in a row, so such a
+// group's address is one scalar and the lane's offset in it never changes;
+// smaller pages, and queries and outputs off a 16-byte boundary, take the
+// GENERAL form with an address a lane and element accesses.
+template <typename T, int HD, int NB, bool GENERAL>
+struct Wave;
+
+// The group of 16 cache rows that begins with key 16 g of a tile.
+template <typename T, int HD>
+__device__ __forceinline__ const char *group_at(const void *base, uint32_t rows, int g) {
+  const uint32_t r = (uint32_t)__builtin_amdgcn_readlane((int)rows, 16 * g);
+  return (const char *)base + (uint64_t)r * (HD * sizeof(T));
+}
+// The cache row of key j (any lane's choice of j).
+template <typename T, int HD>
+__device__ __forceinline__ const char *row_at(const void *base, uint32_t rows, int j) {
+  return (const char *)base + (uint64_t)(uint32_t)__shfl((int)rows, j, 64) * (HD * sizeof(T));
 }
 
-// fp32: 32 keys at cache rows `mine` (lanes 0 .. 31), on the fp32 matrix
-// instructions.  A key lane holds dimensions 4 grp .. + 3 of each 16, so one
-// 16-byte load feeds four k-steps; a value lane holds W neighbouring
-// dimensions of one key, each the row of another 16-dimension tile, so values
-// need no transposition: tile (b, e) holds the dimensions 16 W b + W i + e.
-template <int HD, int NB>
-__device__ __forceinline__ void keys_f32(const PagedAttnArgs &a, uint32_t mine, int nb_used,
-                                         const pf_f32x4 (&qf)[NB][HD / 16], float scale2, WaveState<HD, NB> &w) {
-  constexpr int DT = HD / 16, W = HD >= 64 ? 4 : 2, VB = HD / (16 * W);
-  typedef __attribute__((ext_vector_type(W))) float vecw;
-  const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
-  const unsigned long long mask = __ballot(lane < 32 && mine != kNoRow);
-  if (mask == 0) return;
-  const bool full = mask == 0xffffffffull;
-  const uint32_t at = mine == kNoRow ? 0u : mine;
-  const float *kp = (const float *)a.k + 4 * grp, *vp = (const float *)a.v + W * r16;
-  pf_f32x4 kf[2][DT];
-  vecw vv[2][4][VB];
+// bf16: a tile is a unit.  Keys and values come as whole rows, 1 KB a load
+// (keys in fragment order are sixteen 64-byte pieces, 4 % slower), and go
+// through LDS: keys are read back as fragments, values transposed.
+template <int HD, int NB, bool GENERAL>
+struct Wave<uint16_t, HD, NB, GENERAL> {
+  static constexpr int TK = 64, NT = 4, KS = HD / 32, DT = HD / 16, V4 = HD / 8, RPI = 64 / V4;
+  pf_bf16x8 q[NB][KS];
+  // Two column blocks of 128 dimensions leave room for a tile's keys or its
+  // values on their way, not both: then both use k, in turns.
+  static constexpr bool kTurns = HD * NB > 128;
+  uint4 k[V4], v[kTurns ? 1 : V4];
+  pf_f32x4 o[NB][DT];
+
+  // a column's query, from `src` (null: none)
+  __device__ __forceinline__ void load_q(int nb, const uint16_t *src) {
+    const int grp = (threadIdx.x & 63) >> 4;
 #pragma unroll
-  for (int nt = 0; nt < 2; ++nt) {
-    const float *row = kp + (size_t)(uint32_t)__shfl((int)at, nt * 16 + r16, 64) * HD;
+    for (int st = 0; st < KS; ++st) {
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (src != nullptr) {
+        if constexpr (!GENERAL) {
+          x = *(const uint4 *)(src + st * 32 + grp * 8);
+        } else {
+          uint16_t e[8];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) kf[nt][t] = *(const pf_f32x4 *)(row + 16 * t);
-  }
-#pragma unroll
-  for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float *row = vp + (size_t)(uint32_t)__shfl((int)at, nt * 16 + 4 * grp + i, 64) * HD;
-#pragma unroll
-      for (int b = 0; b < VB; ++b) vv[nt][i][b] = *(const vecw *)(row + 16 * W * b);
-    }
-  if (!full) {
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int b = 0; b < VB; ++b)
-          if (!(mask >> (nt * 16 + 4 * grp + i) & 1)) vv[nt][i][b] = (vecw)0.f;
-  }
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    if (nb < nb_used) {
-      pf_f32x4 sc[2];
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        sc[nt] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            sc[nt] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[nt][t][e], qf[nb][t][e], sc[nt], 0, 0, 0);
+          for (int i = 0; i < 8; ++i) e[i] = src[st * 32 + grp * 8 + i];
+          __builtin_memcpy(&x, e, 16);
+        }
       }
-      const float shrink = soften<2>(sc, mask, full, scale2, w.m[nb], w.l[nb]);
+      q[nb][st] = __builtin_bit_cast(pf_bf16x8, x);
+    }
+  }
+  __device__ __forceinline__ static void load(const void *base, uint32_t rows, uint4 (&x)[V4]) {
+    const int lane = threadIdx.x & 63;
+    const uint32_t off = GENERAL ? (lane % V4) * 16 : (lane / V4) * (HD * 2) + (lane % V4) * 16;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) w.o[nb][dt] *= shrink;
+    for (int c = 0; c < V4; ++c) {
+      if constexpr (GENERAL) {
+        x[c] = *(const uint4 *)(row_at<uint16_t, HD>(base, rows, c * RPI + lane / V4) + off);
+      } else {
+        const int key = c * RPI;          // RPI <= 16 rows of one group
+        x[c] = *(const uint4 *)(group_at<uint16_t, HD>(base, rows, key / 16) + off + (key % 16) * (HD * 2));
+      }
+    }
+  }
+  __device__ __forceinline__ static void stage(const uint4 (&x)[V4], Lds<uint16_t, HD> &lds) {
+    const int lane = threadIdx.x & 63;
+    uint16_t *to = &lds.v[lane / V4][(lane % V4) * 8];       // the rest are constants of the instructions
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+    for (int c = 0; c < V4; ++c) *(uint4 *)(to + c * RPI * (HD + 16)) = x[c];
+    wave_lds_sync();
+  }
+  __device__ __forceinline__ void load_k(const void *base, uint32_t rows) { load(base, rows, k); }
+  __device__ __forceinline__ void load_v(const void *base, uint32_t rows) {
+    if constexpr (kTurns) load(base, rows, k);
+    else load(base, rows, v);
+  }
+  __device__ __forceinline__ void stage_k(Lds<uint16_t, HD> &lds) const { stage(k, lds); }
+  __device__ __forceinline__ void scores(int nb_used, pf_f32x4 (&sc)[NB][NT], const Lds<uint16_t, HD> &lds) const {
+    const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
+    const uint16_t *from = &lds.v[r16][grp * 8];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      pf_bf16x8 kf[KS];
+#pragma unroll
+      for (int st = 0; st < KS; ++st) kf[st] = *(const pf_bf16x8 *)(from + nt * 16 * (HD + 16) + st * 32);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+        if (nb < nb_used) {
+          sc[nb][nt] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int st = 0; st < KS; ++st)
+            sc[nb][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[st], q[nb][st], sc[nb][nt], 0, 0, 0);
+        }
+    }
+  }
+  // values to LDS, those of absent keys as zeros (0 times NaN is not 0)
+  __device__ __forceinline__ void stage_v(unsigned long long mask, bool full, Lds<uint16_t, HD> &lds) {
+    if constexpr (kTurns) stage_masked(k, mask, full, lds);
+    else stage_masked(v, mask, full, lds);
+  }
+  __device__ __forceinline__ static void stage_masked(uint4 (&x)[V4], unsigned long long mask, bool full,
+                                                      Lds<uint16_t, HD> &lds) {
+    if (!full) {
+      const unsigned long long mine = mask >> ((threadIdx.x & 63) / V4);
+#pragma unroll
+      for (int c = 0; c < V4; ++c)
+        if (!(mine >> (c * RPI) & 1)) x[c] = make_uint4(0, 0, 0, 0);
+    }
+    stage(x, lds);
+  }
+  __device__ __forceinline__ void outputs(int nb, const pf_f32x4 (&p)[NT], const Lds<uint16_t, HD> &lds) {
+    const int lane = threadIdx.x & 63, tq = lane >> 4, ti = (lane & 15) >> 2, tg = lane & 3;
+    const uint16_t *from = &lds.v[4 * tq + ti][4 * tg];
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float a = p[2 * st + i / 2][2 * (i % 2)], b = p[2 * st + i / 2][2 * (i % 2) + 1];
+        hi[i] = pf_pack_bf16(a, b);
+        lo[i] = pf_pack_bf16(a - __uint_as_float(hi[i] << 16), b - __uint_as_float(hi[i] & 0xffff0000u));
+      }
+      const pf_bf16x8 ph = __builtin_bit_cast(pf_bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+      const pf_bf16x8 pl = __builtin_bit_cast(pf_bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const pf_bf16x8 vf = tr_frag(from + 32 * st * (HD + 16) + 16 * dt, from + (32 * st + 16) * (HD + 16) + 16 * dt);
+        o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph, o[nb][dt], 0, 0, 0);
+        o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl, o[nb][dt], 0, 0, 0);
+        // not all of the tile's reads at once: the next tile is in registers
+        if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  // dimension of o[.][dt][i]: four neighbours in a register
+  static constexpr int kRun = 4;
+  __device__ __forceinline__ static int dim(int dt, int i) { return 16 * dt + 4 * ((threadIdx.x & 63) >> 4) + i; }
+};
+
+// fp32, on the fp32 matrix instructions: a tile is half a unit.  A key lane
+// holds dimensions 4 grp .. + 3 of each 16, so one 16-byte load feeds four
+// k-steps; a value lane holds W neighbouring dimensions of one key, each the
+// row of another 16-dimension tile, so values need no transposition: tile
+// (b, e) holds the dimensions 16 W b + W i + e.
+template <int HD, int NB, bool GENERAL>
+struct Wave<float, HD, NB, GENERAL> {
+  static constexpr int TK = 32, NT = 2, DT = HD / 16, W = HD >= 64 ? 4 : 2, VB = HD / (16 * W);
+  typedef __attribute__((ext_vector_type(W))) float vecw;
+  static constexpr bool kTurns = false;
+  pf_f32x4 q[NB][DT], k[NT][DT];
+  vecw v[NT][4][VB];
+  pf_f32x4 o[NB][DT];
+
+  __device__ __forceinline__ void load_q(int nb, const float *src) {
+    const int grp = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      pf_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+      if (src != nullptr) {
+        if constexpr (!GENERAL) {
+          x = *(const pf_f32x4 *)(src + t * 16 + grp * 4);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = src[t * 16 + grp * 4 + i];
+        }
+      }
+      q[nb][t] = x;
+    }
+  }
+  __device__ __forceinline__ void load_k(const void *base, uint32_t rows) {
+    const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
+    const uint32_t off = GENERAL ? grp * 16 : r16 * (HD * 4) + grp * 16;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const char *p = GENERAL ? row_at<float, HD>(base, rows, nt * 16 + r16) : group_at<float, HD>(base, rows, nt);
+#pragma unroll
+      for (int t = 0; t < DT; ++t) k[nt][t] = *(const pf_f32x4 *)(p + off + t * 64);
+    }
+  }
+  __device__ __forceinline__ void load_v(const void *base, uint32_t rows) {
+    const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
+    const uint32_t off = GENERAL ? r16 * (W * 4) : 4 * grp * (HD * 4) + r16 * (W * 4);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const char *p = GENERAL ? row_at<float, HD>(base, rows, nt * 16 + 4 * grp + i)
+                               : group_at<float, HD>(base, rows, nt) + i * (HD * 4);
+#pragma unroll
+        for (int b = 0; b < VB; ++b) v[nt][i][b] = *(const vecw *)(p + off + b * (64 * W));
+      }
+  }
+  __device__ __forceinline__ void stage_k(Lds<float, HD> &) const {}
+  __device__ __forceinline__ void scores(int nb_used, pf_f32x4 (&sc)[NB][NT], const Lds<float, HD> &) const {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+      if (nb < nb_used) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          sc[nb][nt] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              sc[nb][nt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[nt][t][e], q[nb][t][e], sc[nb][nt], 0, 0, 0);
+        }
+      }
+  }
+  __device__ __forceinline__ void stage_v(unsigned long long mask, bool full, Lds<float, HD> &) {
+    if (!full) {
+      const unsigned long long mine = mask >> (4 * ((threadIdx.x & 63) >> 4));
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int b = 0; b < VB; ++b)
-#pragma unroll
-            for (int e = 0; e < W; ++e)
-              w.o[nb][b * W + e] =
-                  __builtin_amdgcn_mfma_f32_16x16x4f32(vv[nt][i][b][e], sc[nt][i], w.o[nb][b * W + e], 0, 0, 0);
+            if (!(mine >> (nt * 16 + i) & 1)) v[nt][i][b] = (vecw)0.f;
     }
   }
-}
+  __device__ __forceinline__ void outputs(int nb, const pf_f32x4 (&p)[NT], const Lds<float, HD> &) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int b = 0; b < VB; ++b)
+#pragma unroll
+          for (int e = 0; e < W; ++e)
+            o[nb][b * W + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[nt][i][b][e], p[nt][i], o[nb][b * W + e], 0, 0, 0);
+  }
+  static constexpr int kRun = 1;
+  __device__ __forceinline__ static int dim(int dt, int i) {
+    return 16 * W * (dt / W) + W * (4 * ((threadIdx.x & 63) >> 4) + i) + dt % W;
+  }
+};
 
-// Where a row's records lie: [rows][heads][splits] of head_dim floats, then
-// the statistics of (m, l).
+template <typename T>
+__device__ __forceinline__ void put(T *p, float v) {
+  if constexpr (sizeof(T) == 2) *p = __builtin_bit_cast(uint16_t, (__bf16)v);
+  else *p = v;
+}
+// What a sum over l is multiplied by: a NaN as it is, nothing as 0.
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l != l ? l : 0.f; }
+__device__ __forceinline__ float log_sum(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * kLn2; }
+
+// Records: [rows][heads][smax] of HD floats, then (m, l) of each.
 __device__ __forceinline__ size_t rec_index(const PagedAttnArgs &a, int row, int head, int split, int smax) {
   return ((size_t)row * a.n_heads + head) * smax + split;
 }
 
-template <typename T, int HD, int NB>
-__global__ __launch_bounds__(PA_THREADS) void paged_attn_kernel(PagedAttnArgs a, int smax, float *rec, float2 *stat) {
-  constexpr int TK = sizeof(T) == 2 ? 64 : 32;          // keys of a wave's tile
-  constexpr int TILES = PA_SPLIT / (PA_WAVES * TK);
-  __shared__ Lds<T, HD> lds[PA_WAVES];
-  __shared__ int first_item[PA_ROWS];                   // items before a row's
+// The keys row r attends to: 0 where its sequence is none.
+__device__ __forceinline__ int row_keys(const PagedAttnArgs &a, int r) {
+  const int s = a.seq != nullptr ? a.seq[r] : r;
+  const int n = min(min(a.len[r], a.max_len), a.map.max_pages << a.map.shift);
+  return s >= 0 && s < a.map.n_seqs && n > 0 ? n : 0;
+}
+
+// Four neighbouring dimensions of a row's output, and its lse.
+template <typename T, bool GENERAL>
+__device__ __forceinline__ void finish(const PagedAttnArgs &a, int row, int head, int d, const pf_f32x4 &o, float m,
+                                       float l) {
+  const float inv = inverse(l);
+  T *out = (T *)a.out + (int64_t)row * a.out_row + (int64_t)head * a.out_head + d;
+  if constexpr (!GENERAL) {
+    rec_store4(out, o * inv);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put(out + i, o[i] * inv);
+  }
+  if (d == 0 && a.lse != nullptr) a.lse[(size_t)row * a.n_heads + head] = log_sum(m, l);
+}
+// Rows of a group (group_rows of them, from a leader on) that share leading
+// splits: share[r] is how many the leader takes for all of them.
+struct Sharing {
+  int group, rows;                        // the caller's group; rows a leader takes along
+  const int *share;                       // null: none
+};
+__device__ __forceinline__ int place_in_group(const Sharing &g, int r) { return r % g.group % g.rows; }
+__device__ __forceinline__ int group_rows(const Sharing &g, int r, int n_rows) {   // r a leader
+  return min(min(g.rows, g.group - r % g.group), n_rows - r);
+}
+
+// The leading splits that are the same keys for every row of a group: one
+// workgroup compares their table rows.  They are the same work only where all
+// rows are cut alike and see all of the split, or all have one length.
+__global__ __launch_bounds__(PA_THREADS) void paged_share_kernel(PagedAttnArgs a, Sharing g, int *share) {
+  __shared__ int lens[PA_COLS], seqs[PA_COLS], first;
+  const int tid = threadIdx.x, parts = (g.group + g.rows - 1) / g.rows;
+  const int r0 = blockIdx.x / parts * g.group + blockIdx.x % parts * g.rows;
+  if (r0 >= a.n_rows) return;
+  const int nr = group_rows(g, r0, a.n_rows);
+  if (tid < nr) {
+    lens[tid] = row_keys(a, r0 + tid);
+    seqs[tid] = a.seq != nullptr ? a.seq[r0 + tid] : r0 + tid;
+  }
+  __syncthreads();
+  const int len = lens[0];
+  const RowPlan pl = row_plan(len, a.window);
+  int least = len;
+  bool alike = nr > 1 && len > 0, equal = true;
+  for (int i = 1; i < nr; ++i) {
+    const int n = lens[i];
+    const RowPlan p = row_plan(n, a.window);
+    least = min(least, n);
+    equal = equal && n == len;
+    alike = alike && n > 0 && p.shift == pl.shift && p.lo == pl.lo;
+  }
+  int n_share = 0;
+  if (alike) {
+    // the first column of the table where a row differs
+    const int c0 = (pl.unit0 * PA_UNIT) >> a.map.shift, c1 = (least + (1 << a.map.shift) - 1) >> a.map.shift;
+    if (tid == 0) first = c1;
+    __syncthreads();
+    int mine = c1;
+    for (int c = c0 + tid; c < mine; c += PA_THREADS) {
+      const int p = a.map.table[(size_t)seqs[0] * a.map.max_pages + c];
+      bool differs = false;
+#pragma unroll 4
+      for (int i = 1; i < nr; ++i) differs |= a.map.table[(size_t)seqs[i] * a.map.max_pages + c] != p;
+      if (differs) mine = c;
+    }
+    if (mine < c1) atomicMin(&first, mine);
+    __syncthreads();
+    // the keys before `until` lie on the same pages
+    const int until = first == c1 ? least : first << a.map.shift;
+    n_share = equal && until == len ? pl.n : max(0, until - pl.unit0 * PA_UNIT) / (kSplitKeys << pl.shift);
+  }
+  if (tid < nr) share[r0 + tid] = n_share;
+}
+
+// Where a workgroup is in its work: a tile of its waves' runs of an item.
+struct Place {
+  int item;                               // >= the number of items: nowhere
+  int row, rows, head, head0, cols, split, seq, lo, len;   // kv head; first query head; heads a row
+  int tile, tiles, key, end;              // of the run; this wave's first key of the tile; the row's end
+  int n;                                  // splits of the row
+};
+
+template <typename T, int HD, int NB, bool GENERAL>
+__global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2) void paged_attn_kernel(PagedAttnArgs a, Sharing g, int smax, float *rec,
+                                                                 float2 *stat) {
+  using W = Wave<T, HD, NB, GENERAL>;
+  constexpr int UNIT_TILES = PA_UNIT / W::TK;
+  __shared__ Lds<T, HD> lds_all[PA_WAVES];
+  __shared__ int first_item[PA_ROWS], keys_of[PA_ROWS], share_of[PA_ROWS];   // items before a row's; its keys
   __shared__ int part[PA_WAVES];
   __shared__ float wm[PA_WAVES][16], wl[PA_WAVES][16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, grp = lane >> 4;
-  const int kv = a.map.n_kv_heads, G = a.n_heads / kv, cap = a.max_len;
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Lds<T, HD> &lds = lds_all[wave];
+  const int kv = a.map.n_kv_heads, G = a.n_heads / kv;
+  const int chunks = (G + PA_COLS - 1) / PA_COLS, per_split = kv * chunks;   // items of a split
   const float scale2 = a.scale * kLog2e;
-  auto row_len = [&](int r) {
-    const int s = a.seq != nullptr ? a.seq[r] : r;
-    const int n = min(a.len[r], cap);
-    return s >= 0 && s < a.map.n_seqs && n > 0 ? n : 0;
-  };
   // number the items: every row's splits, the kv heads of a split together
   int items;
   {
@@ -279,8 +473,13 @@ __global__ __launch_bounds__(PA_THREADS) void paged_attn_kernel(PagedAttnArgs a,
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const int r = tid * PER + k;
-      int f;
-      n[k] = r < a.n_rows ? row_splits(row_len(r), a.window, &f) * kv : 0;
+      const int len = r < a.n_rows ? row_keys(a, r) : 0;
+      const int sh = g.share != nullptr && r < a.n_rows ? g.share[r] : 0;
+      keys_of[r] = len;
+      share_of[r] = sh;
+      int c = row_plan(len, a.window).n;
+      if (sh > 0 && place_in_group(g, r) > 0) c -= sh;
+      n[k] = r < a.n_rows ? c * per_split : 0;
       sum += n[k];
     }
     int x = sum;
@@ -305,177 +504,238 @@ __global__ __launch_bounds__(PA_THREADS) void paged_attn_kernel(PagedAttnArgs a,
     }
     __syncthreads();
   }
-  for (int it = blockIdx.x; it < items; it += gridDim.x) {
-    int lo_r = 0, hi_r = a.n_rows - 1;
-    while (lo_r < hi_r) {
-      const int mid = (lo_r + hi_r + 1) >> 1;
-      if (first_item[mid] <= it) lo_r = mid;
-      else hi_r = mid - 1;
+  items = __builtin_amdgcn_readfirstlane(items);
+  auto begin = [&](Place &p) {            // the item's first tile
+    int lo = 0, hi = a.n_rows - 1;
+    while (lo < hi) {                     // the last row with items at or before this one
+      const int mid = (lo + hi + 1) >> 1;
+      if (__builtin_amdgcn_readfirstlane(first_item[mid]) <= p.item) lo = mid;
+      else hi = mid - 1;
     }
-    const int row = lo_r, rem = it - first_item[row];
-    const int h = rem % kv;
-    const int len = row_len(row);
-    const int seq = a.seq != nullptr ? a.seq[row] : row;
-    int split0;
-    const int n_splits = row_splits(len, a.window, &split0), sp = rem / kv;
-    const int lo = a.window > 0 ? max(0, len - a.window) : 0;
-    const int k0 = (split0 + sp) * PA_SPLIT + wave * (PA_SPLIT / PA_WAVES);
-    const int nb_used = (G + 15) / 16;
-    WaveState<HD, NB> w;
+    p.row = lo;
+    const int rem = p.item - __builtin_amdgcn_readfirstlane(first_item[lo]);
+    p.len = __builtin_amdgcn_readfirstlane(keys_of[lo]);
+    p.split = rem / per_split;
+    const int hc = rem - p.split * per_split, chunk = hc / kv;
+    p.head = hc - chunk * kv;
+    p.head0 = p.head * G + chunk * PA_COLS;
+    p.cols = min(PA_COLS, G - chunk * PA_COLS);
+    p.rows = 1;
+    const int sh = __builtin_amdgcn_readfirstlane(share_of[lo]);
+    if (sh > 0) {
+      if (place_in_group(g, lo) > 0) p.split += sh;
+      else if (p.split < sh) p.rows = group_rows(g, lo, a.n_rows);
+    }
+    p.seq = a.seq != nullptr ? __builtin_amdgcn_readfirstlane(a.seq[lo]) : lo;
+    const RowPlan pl = row_plan(p.len, a.window);
+    p.lo = pl.lo;
+    p.n = pl.n;
+    p.tile = 0;
+    p.tiles = UNIT_TILES << pl.shift;
+    p.key = (pl.unit0 + ((p.split * PA_WAVES + wave) << pl.shift)) * PA_UNIT;
+    p.end = (pl.unit0 + pl.units) * PA_UNIT;
+  };
+  auto next = [&](Place &p) {             // the tile after p
+    p.key += W::TK;
+    if (++p.tile < p.tiles) return;
+    p.item += gridDim.x;
+    if (p.item < items) begin(p);
+  };
+  // the cache rows of a tile's keys; which of them the row attends to
+  auto look = [&](const Place &p) -> uint32_t {
+    if (p.item >= items || p.len == 0 || p.key >= p.end) return kNoRow;
+    return page_row(a.map, p.seq, p.key + (lane & (W::TK - 1)), p.head);
+  };
+  auto seen = [&](const Place &p, uint32_t r) -> unsigned long long {
+    const int key = p.key + lane;
+    return __ballot(lane < W::TK && key >= p.lo && key < p.len && r != kNoRow);
+  };
+  auto there = [](uint32_t r) { return r == kNoRow ? 0u : r; };
+  Place cur;
+  cur.item = blockIdx.x;
+  if (cur.item >= items) return;
+  W w;
+  float m[NB], l[NB];
+  // column c of an item: query head head0 + c % cols of row row + c / cols
+  auto query = [&](const Place &p) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      w.m[nb] = -INFINITY;
-      w.l[nb] = 0.f;
-#pragma unroll
-      for (int dt = 0; dt < HD / 16; ++dt) w.o[nb][dt] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
+      const int c = nb * 16 + r16, i = c / p.cols;
+      const T *src = (const T *)a.q + (int64_t)(p.row + i) * a.q_row + (int64_t)(p.head0 + c - i * p.cols) * a.q_head;
+      w.load_q(nb, i < p.rows ? src : nullptr);
     }
-    const T *qrow = (const T *)a.q + (int64_t)row * a.q_row + (int64_t)(h * G) * a.q_head;
-    auto cache_row = [&](int key) {
-      return key >= lo && key < len ? page_row(a.map, seq, key, h) : kNoRow;
-    };
-    if constexpr (sizeof(T) == 2) {
-      pf_bf16x8 qf[NB][HD / 32];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const int p = nb * 16 + r16;
-#pragma unroll
-        for (int st = 0; st < HD / 32; ++st) {
-          uint16_t x[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = p < G ? qrow[(int64_t)p * a.q_head + st * 32 + grp * 8 + i] : 0;
-          __builtin_memcpy(&qf[nb][st], x, 16);
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < TILES; ++t) keys_bf16<HD, NB>(a, cache_row(k0 + t * TK + lane), nb_used, qf, scale2, lds[wave], w);
-    } else {
-      pf_f32x4 qf[NB][HD / 16];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const int p = nb * 16 + r16;
-#pragma unroll
-        for (int t = 0; t < HD / 16; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) qf[nb][t][i] = p < G ? qrow[(int64_t)p * a.q_head + t * 16 + grp * 4 + i] : 0.f;
-      }
-#pragma unroll
-      for (int t = 0; t < TILES; ++t)
-        keys_f32<HD, NB>(a, lane < TK ? cache_row(k0 + t * TK + lane) : kNoRow, nb_used, qf, scale2, w);
-    }
-    // the four waves' sums under one reference, 16 columns at a time
+  };
+  auto clear = [&] {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      if (nb < nb_used) {
-        if (grp == 0) {
-          wm[wave][r16] = w.m[nb];
-          wl[wave][r16] = w.l[nb];
+      m[nb] = -INFINITY;
+      l[nb] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < W::DT; ++dt) w.o[nb][dt] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  begin(cur);
+  uint32_t rows = look(cur);
+  w.load_k(a.k, there(rows));
+  if constexpr (!W::kTurns) w.load_v(a.v, there(rows));
+  query(cur);
+  clear();
+  Place nxt = cur;
+  next(nxt);
+  uint32_t rows1 = look(nxt);
+  for (;;) {
+    // the tile after next is looked up while this one is worked on, and the
+    // next one's keys and values are on their way as soon as registers allow
+    Place far = nxt;
+    if (far.item < items) next(far);
+    const uint32_t rows2 = look(far);
+    const unsigned long long mask = seen(cur, rows);
+    const bool full = mask == (W::TK == 64 ? ~0ull : 0xffffffffull);
+    const int nb_used = (cur.rows * cur.cols + 15) / 16;
+    pf_f32x4 sc[NB][W::NT];
+    const bool last = nxt.item != cur.item;                  // cur is its item's last tile
+    w.stage_k(lds);
+    if constexpr (W::kTurns) w.load_v(a.v, there(rows));
+    w.scores(nb_used, sc, lds);
+    // (without these the scheduler moves loads over the products that free
+    // their registers, and spills)
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (!W::kTurns) w.load_k(a.k, there(rows1));
+    if (last && nxt.item < items) query(nxt);
+    if constexpr (sizeof(T) == 2) wave_lds_sync();           // the keys are read before values take their place
+    w.stage_v(mask, full, lds);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (W::kTurns) w.load_k(a.k, there(rows1));
+    else if constexpr (sizeof(T) == 2) w.load_v(a.v, there(rows1));
+    if (mask != 0) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+        if (nb < nb_used) {
+          const float shrink = soften<W::NT>(sc[nb], mask, full, scale2, m[nb], l[nb]);
+#pragma unroll
+          for (int dt = 0; dt < W::DT; ++dt) w.o[nb][dt] *= shrink;
+          w.outputs(nb, sc[nb], lds);
         }
+    }
+    if constexpr (sizeof(T) == 4) w.load_v(a.v, there(rows1));
+    else wave_lds_sync();                 // the values are read before anything takes their place
+    if (last) {
+      // the four waves' sums under one reference, 16 columns at a time
 #pragma unroll
-        for (int dt = 0; dt < HD / 16; ++dt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            constexpr int W = HD >= 64 ? 4 : 2;
-            const int d = sizeof(T) == 2 ? 16 * dt + 4 * grp + i : 16 * W * (dt / W) + W * (4 * grp + i) + dt % W;
-            lds[wave].o[r16][d] = w.o[nb][dt][i];
+      for (int nb = 0; nb < NB; ++nb) {
+        const int used = min(16, cur.rows * cur.cols - nb * 16);
+        if (used <= 0) break;
+        const float sum = quad_sum(l[nb]);
+        if (r16 < used) {
+          if (grp == 0) {
+            wm[wave][r16] = m[nb];
+            wl[wave][r16] = sum;
           }
-        __syncthreads();
-        const int cols = min(16, G - nb * 16);
-        for (int e = tid; e < cols * HD; e += PA_THREADS) {
-          const int c = e / HD, d = e % HD;
-          float m = wm[0][c];
 #pragma unroll
-          for (int v = 1; v < PA_WAVES; ++v) m = fmaxf(m, wm[v][c]);
-          const float ref = m == -INFINITY ? 0.f : m;
-          float o = 0.f, l = 0.f;
+          for (int dt = 0; dt < W::DT; ++dt) {
+            if constexpr (W::kRun == 4) {
+              *(pf_f32x4 *)&lds.o[r16][W::dim(dt, 0)] = w.o[nb][dt];
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) lds.o[r16][W::dim(dt, i)] = w.o[nb][dt][i];
+            }
+          }
+        }
+        lds_barrier();
+        for (int e = tid; e < used * (HD / 4); e += PA_THREADS) {
+          const int c = e / (HD / 4), d = e % (HD / 4) * 4;
+          float mm = wm[0][c];
+#pragma unroll
+          for (int v = 1; v < PA_WAVES; ++v) mm = fmaxf(mm, wm[v][c]);
+          const float ref = mm == -INFINITY ? 0.f : mm;
+          pf_f32x4 o = {0.f, 0.f, 0.f, 0.f};
+          float ll = 0.f;
 #pragma unroll
           for (int v = 0; v < PA_WAVES; ++v) {
             const float f = __builtin_amdgcn_exp2f(wm[v][c] - ref);
-            o += f * lds[v].o[c][d];
-            l += f * wl[v][c];
+            const pf_f32x4 x = *(const pf_f32x4 *)&lds_all[v].o[c][d];
+            ll = fmaf(f, wl[v][c], ll);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = fmaf(f, x[i], o[i]);
           }
-          const int head = h * G + nb * 16 + c;
-          if (n_splits == 1) {
-            T *out = (T *)a.out + (int64_t)row * a.out_row + (int64_t)head * a.out_head;
-            const float y = l > 0.f ? o / l : l != l ? l : 0.f;
-            if constexpr (sizeof(T) == 2) out[d] = __builtin_bit_cast(uint16_t, (__bf16)y);
-            else out[d] = y;
-            if (d == 0 && a.lse != nullptr) a.lse[(size_t)row * a.n_heads + head] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+          const int col = nb * 16 + c, i = col / cur.cols;
+          const int row = cur.row + i, head = cur.head0 + col - i * cur.cols;
+          if (cur.n == 1) {
+            finish<T, GENERAL>(a, row, head, d, o, mm, ll);
           } else {
-            const size_t at = rec_index(a, row, head, sp, smax);
-            rec[at * HD + d] = o;
-            if (d == 0) stat[at] = make_float2(m, l);
+            const size_t at = rec_index(a, row, head, cur.split, smax);
+            *(pf_f32x4 *)(rec + at * HD + d) = o;
+            if (d == 0) stat[at] = make_float2(mm, ll);
           }
         }
-        __syncthreads();
+        lds_barrier();
       }
+      if (nxt.item >= items) break;
+      clear();
     }
+    cur = nxt;
+    nxt = far;
+    rows = rows1;
+    rows1 = rows2;
   }
 }
 
-// A row's records, added in order: a workgroup a (row, query head), HD / 4
-// lanes a record.
-template <typename T, int HD>
+// A row's records together: HD / 4 lanes a record, AT records at a time (record
+// j with the others j % AT), then the AT sums in order.  A workgroup is a
+// (row, query head); every record is requested before the statistics are in.
+template <typename T, int HD, bool GENERAL>
 __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedAttnArgs a, int smax, const float *rec,
                                                               const float2 *stat) {
-  constexpr int LPR = HD / 4, AT = PA_THREADS / LPR;    // records at a time
-  __shared__ float4 sum[AT][LPR];
+  constexpr int LPR = HD / 4, AT = PA_THREADS / LPR, PER = (PA_SPLITS + AT - 1) / AT;
+  __shared__ pf_f32x4 sums[AT][LPR];
   __shared__ float lsum[AT];
   const int row = blockIdx.x / a.n_heads, head = blockIdx.x - row * a.n_heads;
-  const int s = a.seq != nullptr ? a.seq[row] : row;
-  const int n0 = min(a.len[row], a.max_len);
-  if (s < 0 || s >= a.map.n_seqs || n0 <= 0) return;
-  int split0;
-  const int n = row_splits(n0, a.window, &split0);
+  const int n = row_plan(row_keys(a, row), a.window).n;
   if (n == 1) return;
-  const int tid = threadIdx.x, j0 = tid / LPR, d = tid % LPR;
+  const int tid = threadIdx.x, lane = tid & 63, j0 = tid / LPR, d = tid % LPR;
   const size_t base = rec_index(a, row, head, 0, smax);
-  float m = -INFINITY;
-  for (int j = 0; j < n; ++j) m = fmaxf(m, stat[base + j].x);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float l = 0.f;
-  for (int j = j0; j < n; j += AT) {
-    const float2 st = stat[base + j];
-    const float4 x = *(const float4 *)(rec + (base + j) * HD + 4 * d);
-    const float f = __builtin_amdgcn_exp2f(st.x - ref);
-    l += f * st.y;
-    o.x += f * x.x;
-    o.y += f * x.y;
-    o.z += f * x.z;
-    o.w += f * x.w;
+  const float2 mine = lane < n ? stat[base + lane] : make_float2(-INFINITY, 0.f);
+  pf_f32x4 x[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int j = j0 + k * AT;
+    x[k] = j < n ? *(const pf_f32x4 *)(rec + (base + j) * HD + 4 * d) : pf_f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  sum[j0][d] = o;
+  const float m = wave_max(mine.x);
+  const float factor = __builtin_amdgcn_exp2f(mine.x - (m == -INFINITY ? 0.f : m));
+  pf_f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const float f = __shfl(factor, j0 + k * AT, 64), lj = __shfl(mine.y, j0 + k * AT, 64);
+    if (j0 + k * AT < n) {
+      l = fmaf(f, lj, l);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = fmaf(f, x[k][i], o[i]);
+    }
+  }
+  sums[j0][d] = o;
   if (d == 0) lsum[j0] = l;
   __syncthreads();
   if (j0 != 0) return;
 #pragma unroll
   for (int k = 1; k < AT; ++k) {
-    const float4 x = sum[k][d];
-    o.x += x.x;
-    o.y += x.y;
-    o.z += x.z;
-    o.w += x.w;
+    o += sums[k][d];
     l += lsum[k];
   }
-  const float y[4] = {o.x, o.y, o.z, o.w};
-  T *out = (T *)a.out + (int64_t)row * a.out_row + (int64_t)head * a.out_head + 4 * d;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float v = l > 0.f ? y[i] / l : l != l ? l : 0.f;
-    if constexpr (sizeof(T) == 2) out[i] = __builtin_bit_cast(uint16_t, (__bf16)v);
-    else out[i] = v;
-  }
-  if (d == 0 && a.lse != nullptr) a.lse[(size_t)row * a.n_heads + head] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+  finish<T, GENERAL>(a, row, head, 4 * d, o, m, l);
 }
 
-int max_splits(int max_len) { return std::max(1, (max_len + PA_SPLIT - 1) / PA_SPLIT); }
+int max_splits(int max_len) { return std::max(1, std::min(PA_SPLITS, (max_len + kSplitKeys - 1) / kSplitKeys)); }
 
-template <typename T, int HD, int NB>
-hipError_t go(const PagedAttnArgs &a, hipStream_t s) {
+// The call's rows in launches of at most PA_ROWS.
+template <typename T, int HD, int NB, bool GENERAL>
+hipError_t go(const PagedAttnArgs &a, int rows_along, hipStream_t s) {
   const int smax = max_splits(a.max_len);
-  for (int r0 = 0; r0 < a.n_rows; r0 += PA_ROWS) {
+  const int group = std::min(a.group, PA_ROWS), at_once = PA_ROWS / group * group;
+  for (int r0 = 0; r0 < a.n_rows; r0 += at_once) {
     PagedAttnArgs b = a;
-    b.n_rows = std::min(PA_ROWS, a.n_rows - r0);
+    b.n_rows = std::min(at_once, a.n_rows - r0);
     b.q = (const T *)a.q + r0 * a.q_row;
     b.out = (T *)a.out + r0 * a.out_row;
     b.len = a.len + r0;
@@ -484,12 +744,25 @@ hipError_t go(const PagedAttnArgs &a, hipStream_t s) {
     else b.map.table = a.map.table + (size_t)r0 * a.map.max_pages, b.map.n_seqs = std::max(0, a.map.n_seqs - r0);
     float *rec = (float *)a.work;
     float2 *stat = (float2 *)(rec + (size_t)std::min(a.n_rows, PA_ROWS) * a.n_heads * smax * HD);
-    const int64_t most = (int64_t)b.n_rows * a.map.n_kv_heads * smax;
-    paged_attn_kernel<T, HD, NB><<<(unsigned)std::min<int64_t>(most, 1024), PA_THREADS, 0, s>>>(b, smax, rec, stat);
-    hipError_t e = hipGetLastError();
+    Sharing g{group, rows_along, nullptr};
+    hipError_t e;
+    const int chunks = (a.n_heads / a.map.n_kv_heads + PA_COLS - 1) / PA_COLS;
+    const int64_t row_items = (int64_t)b.n_rows * a.map.n_kv_heads * chunks;
+    if (rows_along > 1) {
+      int *share = (int *)(stat + (size_t)std::min(a.n_rows, PA_ROWS) * a.n_heads * smax);
+      const int parts = (group + rows_along - 1) / rows_along;
+      paged_share_kernel<<<(b.n_rows + group - 1) / group * parts, PA_THREADS, 0, s>>>(b, g, share);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      g.share = share;
+    }
+    // two workgroups fit a compute unit; further items wait their turn in them
+    paged_attn_kernel<T, HD, NB, GENERAL>
+        <<<(unsigned)std::min<int64_t>(row_items * smax, 512), PA_THREADS, 0, s>>>(b, g, smax, rec, stat);
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (smax > 1) {
-      paged_join_kernel<T, HD><<<b.n_rows * a.n_heads, PA_THREADS, 0, s>>>(b, smax, rec, stat);
+      paged_join_kernel<T, HD, GENERAL><<<b.n_rows * a.n_heads, PA_THREADS, 0, s>>>(b, smax, rec, stat);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
@@ -498,24 +771,33 @@ hipError_t go(const PagedAttnArgs &a, hipStream_t s) {
 }
 
 template <typename T, int HD>
-hipError_t go_nb(const PagedAttnArgs &a, hipStream_t s) {
-  const int g = a.n_heads / a.map.n_kv_heads;
-  return g <= 16 ? go<T, HD, 1>(a, s) : g <= 32 ? go<T, HD, 2>(a, s) : go<T, HD, 4>(a, s);
+hipError_t go_hd(const PagedAttnArgs &a, hipStream_t s) {
+  auto whole = [](const void *p, int64_t row, int64_t head) {
+    return (uintptr_t)p % 16 == 0 && row * sizeof(T) % 16 == 0 && head * sizeof(T) % 16 == 0;
+  };
+  const bool plain = a.map.shift >= 4 && whole(a.q, a.q_row, a.q_head) && whole(a.out, a.out_row, a.out_head);
+  const int G = a.n_heads / a.map.n_kv_heads;
+  // rows whose query heads fill the columns of an item together
+  const int along = std::max(1, std::min(std::min(a.group, a.n_rows), PA_COLS / G));
+  if (std::min(G, PA_COLS) * along <= 16)
+    return plain ? go<T, HD, 1, false>(a, along, s) : go<T, HD, 1, true>(a, along, s);
+  return plain ? go<T, HD, 2, false>(a, along, s) : go<T, HD, 2, true>(a, along, s);
 }
 
 }  // namespace
 
-size_t paged_attention_work(int n_rows, int n_heads, int head_dim, int max_len) {
+size_t paged_attention_work(int n_rows, int n_heads, int head_dim, int max_len, int group) {
   const int smax = max_splits(max_len);
-  if (smax == 1) return 0;
-  return (size_t)std::min(n_rows, PA_ROWS) * n_heads * smax * (head_dim + 2) * sizeof(float);
+  if (smax == 1 && group == 1) return 0;
+  const size_t rows = std::min(n_rows, PA_ROWS);
+  return rows * n_heads * smax * (head_dim + 2) * sizeof(float) + rows * sizeof(int);
 }
 
 hipError_t launch_paged_attention(int dtype, const PagedAttnArgs &a, hipStream_t s) {
   if (dtype == DEX_F32)
-    return a.head_dim == 32 ? go_nb<float, 32>(a, s) : a.head_dim == 64 ? go_nb<float, 64>(a, s) : go_nb<float, 128>(a, s);
-  return a.head_dim == 32 ? go_nb<uint16_t, 32>(a, s)
-                          : a.head_dim == 64 ? go_nb<uint16_t, 64>(a, s) : go_nb<uint16_t, 128>(a, s);
+    return a.head_dim == 32 ? go_hd<float, 32>(a, s) : a.head_dim == 64 ? go_hd<float, 64>(a, s) : go_hd<float, 128>(a, s);
+  return a.head_dim == 32 ? go_hd<uint16_t, 32>(a, s)
+                          : a.head_dim == 64 ? go_hd<uint16_t, 64>(a, s) : go_hd<uint16_t, 128>(a, s);
 }
 
 }  // namespace dex

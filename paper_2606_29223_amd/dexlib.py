@@ -124,7 +124,7 @@ def load(path: str | None = None):
     lib.dex_rope.argtypes = [i32, i32, P(DexRotary), i32, i32, vp, *heads, i32, *heads, *heads, i32, *heads, vp]
     lib.dex_pages_append.argtypes = [i32, i32, P(DexRotary), i32, vp, vp, *heads, i32, *heads, *heads, *heads, i32,
                                      vp, vp, i32, i32, vp, i32, i32, vp]
-    lib.dex_pages_attention_work.argtypes = [i32] * 5
+    lib.dex_pages_attention_work.argtypes = [i32] * 6
     lib.dex_pages_attention.argtypes = [i32, i32, i32, i32, i32, vp, vp, i32, i32, i32, f32, *heads, vp, vp, i32, i32,
                                         vp, i32, i32, *heads, vp, vp, vp]
     lib.dex_pages_fork.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]

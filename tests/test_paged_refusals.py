@@ -28,9 +28,9 @@ ROPE = dict(dtype=1, head_dim=64, plan=PLAN, inverse=0, n_rows=2, pos=FAKE, q=FA
 APPEND = dict(dtype=1, head_dim=64, plan=PLAN, n_rows=2, seq=None, pos=FAKE, q=FAKE, q_row=256, q_head=64, n_heads=4,
               q_out=FAKE, qo_row=256, qo_head=64, k=FAKE, k_row=128, k_head=64, v=FAKE, v_row=128, v_head=64, n_kv=2,
               k_pages=FAKE, v_pages=FAKE, n_pages=8, page_size=16, table=FAKE, n_seqs=2, max_pages=4)
-ATTENTION = dict(dtype=1, head_dim=64, n_heads=4, n_kv=2, n_rows=2, seq=None, lens=FAKE, max_len=600, window=0, group=1,
+ATTENTION = dict(dtype=1, head_dim=64, n_heads=4, n_kv=2, n_rows=2, seq=None, lens=FAKE, max_len=5000, window=0, group=1,
                  scale=0.125, q=FAKE, q_row=256, q_head=64, k_pages=FAKE, v_pages=FAKE, n_pages=80, page_size=16,
-                 table=FAKE, n_seqs=2, max_pages=40, out=FAKE, o_row=256, o_head=64, lse=None, work=FAKE)
+                 table=FAKE, n_seqs=2, max_pages=400, out=FAKE, o_row=256, o_head=64, lse=None, work=FAKE)
 FORK = dict(table=FAKE, ref=FAKE, length=FAKE, parent=FAKE, n_seqs=2, max_pages=4, n_pages=8, t=FAKE, r=FAKE, n=FAKE)
 RESERVE = dict(table=FAKE, ref=FAKE, length=FAKE, n_new=FAKE, n_seqs=2, max_pages=4, n_pages=8, page_size=16, pos=FAKE,
                src=FAKE, dst=FAKE, tokens=FAKE, state=FAKE)
@@ -112,10 +112,10 @@ def test_no_rows_is_no_work(lib):
 
 
 def test_work_sizes(lib):
-    assert lib.dex_pages_attention_work(4, 32, 8, 128, 100) >= 0
-    small, big = (lib.dex_pages_attention_work(4, 32, 8, 128, n) for n in (4096, 65536))
+    assert lib.dex_pages_attention_work(4, 32, 8, 128, 100, 1) == 0
+    small, big = (lib.dex_pages_attention_work(4, 32, 8, 128, n, 2) for n in (1100, 65536))
     assert 0 < small < big
-    assert lib.dex_pages_attention_work(1 << 20, 32, 8, 128, 1 << 20) < 1 << 40      # rows go 1024 at a time
+    assert lib.dex_pages_attention_work(1 << 20, 32, 8, 128, 1 << 20, 1) < 1 << 30   # rows go a few hundred at a time
     assert lib.dex_beam_select_work(1, 2, 4, 500, 4) > 0
     assert lib.dex_beam_select_work(7, 2, 4, 500, 4) == 0
 
