@@ -111,17 +111,18 @@ __device__ __forceinline__ float soften(pf_f32x4 (&sc)[NT], unsigned long long m
 // One wave's work on tiles of TK keys, for 16 NB columns (column r16 of block
 // nb).  `rows` of a tile: lane j holds the cache row of key j, or 0 where its
 // page is none (row 0 is there; what is read for a key that is not attended to
-// is put out).  Pages of 16 keys or more hold 16 neighbours in a row, so such a
-// group's address is one scalar and the lane's offset in it never changes;
-// smaller pages, and queries and outputs off a 16-byte boundary, take the
-// GENERAL form with an address a lane and element accesses.
-template <typename T, int HD, int NB, bool GENERAL>
+// is put out).  RUN neighbouring keys lie in one page, so their address is one
+// scalar and a lane's offset from it never changes: the 4, 8 or 16 keys of a
+// 1 KB load in bf16, 16 in fp32.  RUN 1, for smaller pages and for queries or
+// outputs off a 16-byte boundary, has an address a lane and accesses by
+// elements (16 x 2000 keys of 128 bf16: 50 us against 36).
+template <typename T, int HD, int NB, int RUN>
 struct Wave;
 
-// The group of 16 cache rows that begins with key 16 g of a tile.
+// The cache rows that begin with key j of a tile, the same j for all lanes.
 template <typename T, int HD>
-__device__ __forceinline__ const char *group_at(const void *base, uint32_t rows, int g) {
-  const uint32_t r = (uint32_t)__builtin_amdgcn_readlane((int)rows, 16 * g);
+__device__ __forceinline__ const char *run_at(const void *base, uint32_t rows, int j) {
+  const uint32_t r = (uint32_t)__builtin_amdgcn_readlane((int)rows, j);
   return (const char *)base + (uint64_t)r * (HD * sizeof(T));
 }
 // The cache row of key j (any lane's choice of j).
@@ -133,8 +134,8 @@ __device__ __forceinline__ const char *row_at(const void *base, uint32_t rows, i
 // bf16: a tile is a unit.  Keys and values come as whole rows, 1 KB a load
 // (keys in fragment order are sixteen 64-byte pieces, 4 % slower), and go
 // through LDS: keys are read back as fragments, values transposed.
-template <int HD, int NB, bool GENERAL>
-struct Wave<uint16_t, HD, NB, GENERAL> {
+template <int HD, int NB, int RUN>
+struct Wave<uint16_t, HD, NB, RUN> {
   static constexpr int TK = 64, NT = 4, KS = HD / 32, DT = HD / 16, V4 = HD / 8, RPI = 64 / V4;
   pf_bf16x8 q[NB][KS];
   // Two column blocks of 128 dimensions leave room for a tile's keys or its
@@ -150,7 +151,7 @@ struct Wave<uint16_t, HD, NB, GENERAL> {
     for (int st = 0; st < KS; ++st) {
       uint4 x = make_uint4(0, 0, 0, 0);
       if (src != nullptr) {
-        if constexpr (!GENERAL) {
+        if constexpr (RUN > 1) {
           x = *(const uint4 *)(src + st * 32 + grp * 8);
         } else {
           uint16_t e[8];
@@ -164,14 +165,15 @@ struct Wave<uint16_t, HD, NB, GENERAL> {
   }
   __device__ __forceinline__ static void load(const void *base, uint32_t rows, uint4 (&x)[V4]) {
     const int lane = threadIdx.x & 63;
-    const uint32_t off = GENERAL ? (lane % V4) * 16 : (lane / V4) * (HD * 2) + (lane % V4) * 16;
+    const uint32_t off = RUN == 1 ? (lane % V4) * 16 : (lane / V4) * (HD * 2) + (lane % V4) * 16;
 #pragma unroll
     for (int c = 0; c < V4; ++c) {
-      if constexpr (GENERAL) {
+      if constexpr (RUN == 1) {
         x[c] = *(const uint4 *)(row_at<uint16_t, HD>(base, rows, c * RPI + lane / V4) + off);
       } else {
-        const int key = c * RPI;          // RPI <= 16 rows of one group
-        x[c] = *(const uint4 *)(group_at<uint16_t, HD>(base, rows, key / 16) + off + (key % 16) * (HD * 2));
+        static_assert(RUN % RPI == 0, "a load's rows lie in one run");
+        const int key = c * RPI;
+        x[c] = *(const uint4 *)(run_at<uint16_t, HD>(base, rows, key / RUN * RUN) + off + (key % RUN) * (HD * 2));
       }
     }
   }
@@ -255,8 +257,8 @@ struct Wave<uint16_t, HD, NB, GENERAL> {
 // k-steps; a value lane holds W neighbouring dimensions of one key, each the
 // row of another 16-dimension tile, so values need no transposition: tile
 // (b, e) holds the dimensions 16 W b + W i + e.
-template <int HD, int NB, bool GENERAL>
-struct Wave<float, HD, NB, GENERAL> {
+template <int HD, int NB, int RUN>
+struct Wave<float, HD, NB, RUN> {
   static constexpr int TK = 32, NT = 2, DT = HD / 16, W = HD >= 64 ? 4 : 2, VB = HD / (16 * W);
   typedef __attribute__((ext_vector_type(W))) float vecw;
   static constexpr bool kTurns = false;
@@ -270,7 +272,7 @@ struct Wave<float, HD, NB, GENERAL> {
     for (int t = 0; t < DT; ++t) {
       pf_f32x4 x = {0.f, 0.f, 0.f, 0.f};
       if (src != nullptr) {
-        if constexpr (!GENERAL) {
+        if constexpr (RUN > 1) {
           x = *(const pf_f32x4 *)(src + t * 16 + grp * 4);
         } else {
 #pragma unroll
@@ -282,23 +284,23 @@ struct Wave<float, HD, NB, GENERAL> {
   }
   __device__ __forceinline__ void load_k(const void *base, uint32_t rows) {
     const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
-    const uint32_t off = GENERAL ? grp * 16 : r16 * (HD * 4) + grp * 16;
+    const uint32_t off = RUN == 1 ? grp * 16 : r16 * (HD * 4) + grp * 16;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const char *p = GENERAL ? row_at<float, HD>(base, rows, nt * 16 + r16) : group_at<float, HD>(base, rows, nt);
+      const char *p = RUN == 1 ? row_at<float, HD>(base, rows, nt * 16 + r16) : run_at<float, HD>(base, rows, nt * 16);
 #pragma unroll
       for (int t = 0; t < DT; ++t) k[nt][t] = *(const pf_f32x4 *)(p + off + t * 64);
     }
   }
   __device__ __forceinline__ void load_v(const void *base, uint32_t rows) {
     const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
-    const uint32_t off = GENERAL ? r16 * (W * 4) : 4 * grp * (HD * 4) + r16 * (W * 4);
+    const uint32_t off = RUN == 1 ? r16 * (W * 4) : 4 * grp * (HD * 4) + r16 * (W * 4);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const char *p = GENERAL ? row_at<float, HD>(base, rows, nt * 16 + 4 * grp + i)
-                               : group_at<float, HD>(base, rows, nt) + i * (HD * 4);
+        const char *p = RUN == 1 ? row_at<float, HD>(base, rows, nt * 16 + 4 * grp + i)
+                               : run_at<float, HD>(base, rows, nt * 16) + i * (HD * 4);
 #pragma unroll
         for (int b = 0; b < VB; ++b) v[nt][i][b] = *(const vecw *)(p + off + b * (64 * W));
       }
@@ -370,12 +372,12 @@ __device__ __forceinline__ int row_keys(const PagedAttnArgs &a, int r) {
 }
 
 // Four neighbouring dimensions of a row's output, and its lse.
-template <typename T, bool GENERAL>
+template <typename T, int RUN>
 __device__ __forceinline__ void finish(const PagedAttnArgs &a, int row, int head, int d, const pf_f32x4 &o, float m,
                                        float l) {
   const float inv = inverse(l);
   T *out = (T *)a.out + (int64_t)row * a.out_row + (int64_t)head * a.out_head + d;
-  if constexpr (!GENERAL) {
+  if constexpr (RUN > 1) {
     rec_store4(out, o * inv);
   } else {
 #pragma unroll
@@ -450,10 +452,10 @@ struct Place {
   int n;                                  // splits of the row
 };
 
-template <typename T, int HD, int NB, bool GENERAL>
+template <typename T, int HD, int NB, int RUN>
 __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2) void paged_attn_kernel(PagedAttnArgs a, Sharing g, int smax, float *rec,
                                                                  float2 *stat) {
-  using W = Wave<T, HD, NB, GENERAL>;
+  using W = Wave<T, HD, NB, RUN>;
   constexpr int UNIT_TILES = PA_UNIT / W::TK;
   __shared__ Lds<T, HD> lds_all[PA_WAVES];
   __shared__ int first_item[PA_ROWS], keys_of[PA_ROWS], share_of[PA_ROWS];   // items before a row's; its keys
@@ -661,7 +663,7 @@ __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2
           const int col = nb * 16 + c, i = col / cur.cols;
           const int row = cur.row + i, head = cur.head0 + col - i * cur.cols;
           if (cur.n == 1) {
-            finish<T, GENERAL>(a, row, head, d, o, mm, ll);
+            finish<T, RUN>(a, row, head, d, o, mm, ll);
           } else {
             const size_t at = rec_index(a, row, head, cur.split, smax);
             *(pf_f32x4 *)(rec + at * HD + d) = o;
@@ -683,7 +685,7 @@ __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2
 // A row's records together: HD / 4 lanes a record, AT records at a time (record
 // j with the others j % AT), then the AT sums in order.  A workgroup is a
 // (row, query head); every record is requested before the statistics are in.
-template <typename T, int HD, bool GENERAL>
+template <typename T, int HD, int RUN>
 __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedAttnArgs a, int smax, const float *rec,
                                                               const float2 *stat) {
   constexpr int LPR = HD / 4, AT = PA_THREADS / LPR, PER = (PA_SPLITS + AT - 1) / AT;
@@ -723,13 +725,13 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedAttnArgs a,
     o += sums[k][d];
     l += lsum[k];
   }
-  finish<T, GENERAL>(a, row, head, 4 * d, o, m, l);
+  finish<T, RUN>(a, row, head, 4 * d, o, m, l);
 }
 
 int max_splits(int max_len) { return std::max(1, std::min(PA_SPLITS, (max_len + kSplitKeys - 1) / kSplitKeys)); }
 
 // The call's rows in launches of at most PA_ROWS.
-template <typename T, int HD, int NB, bool GENERAL>
+template <typename T, int HD, int NB, int RUN>
 hipError_t go(const PagedAttnArgs &a, int rows_along, hipStream_t s) {
   const int smax = max_splits(a.max_len);
   const int group = std::min(a.group, PA_ROWS), at_once = PA_ROWS / group * group;
@@ -757,12 +759,12 @@ hipError_t go(const PagedAttnArgs &a, int rows_along, hipStream_t s) {
       g.share = share;
     }
     // two workgroups fit a compute unit; further items wait their turn in them
-    paged_attn_kernel<T, HD, NB, GENERAL>
+    paged_attn_kernel<T, HD, NB, RUN>
         <<<(unsigned)std::min<int64_t>(row_items * smax, 512), PA_THREADS, 0, s>>>(b, g, smax, rec, stat);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (smax > 1) {
-      paged_join_kernel<T, HD, GENERAL><<<b.n_rows * a.n_heads, PA_THREADS, 0, s>>>(b, smax, rec, stat);
+      paged_join_kernel<T, HD, RUN><<<b.n_rows * a.n_heads, PA_THREADS, 0, s>>>(b, smax, rec, stat);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
@@ -775,13 +777,14 @@ hipError_t go_hd(const PagedAttnArgs &a, hipStream_t s) {
   auto whole = [](const void *p, int64_t row, int64_t head) {
     return (uintptr_t)p % 16 == 0 && row * sizeof(T) % 16 == 0 && head * sizeof(T) % 16 == 0;
   };
-  const bool plain = a.map.shift >= 4 && whole(a.q, a.q_row, a.q_head) && whole(a.out, a.out_row, a.out_head);
+  const bool vectors = whole(a.q, a.q_row, a.q_head) && whole(a.out, a.out_row, a.out_head);
   const int G = a.n_heads / a.map.n_kv_heads;
   // rows whose query heads fill the columns of an item together
   const int along = std::max(1, std::min(std::min(a.group, a.n_rows), PA_COLS / G));
-  if (std::min(G, PA_COLS) * along <= 16)
-    return plain ? go<T, HD, 1, false>(a, along, s) : go<T, HD, 1, true>(a, along, s);
-  return plain ? go<T, HD, 2, false>(a, along, s) : go<T, HD, 2, true>(a, along, s);
+  const bool one = std::min(G, PA_COLS) * along <= 16;
+  constexpr int RUN = sizeof(T) == 2 ? 512 / HD : 16;
+  if (vectors && 1 << a.map.shift >= RUN) return one ? go<T, HD, 1, RUN>(a, along, s) : go<T, HD, 2, RUN>(a, along, s);
+  return one ? go<T, HD, 1, 1>(a, along, s) : go<T, HD, 2, 1>(a, along, s);
 }
 
 }  // namespace
