@@ -374,7 +374,7 @@ dex_status dex_debug_copy(void *dst, const void *src, int64_t bytes, void *hip_s
  *     1024.  Position p of sequence s is slot p % page_size of page
  *     table[s][p / page_size] (device int32 [n_seqs][max_pages]); an entry
  *     outside [0, n_pages), -1 by custom, is no page.  n_pages * n_kv_heads *
- *     page_size < 2^32 - 1, n_pages <= 2^30.
+ *     page_size < 2^32 - 1, n_pages <= 2^30, max_pages * page_size <= 2^30.
  *   - All arrays are device memory unless they are called host arrays; all
  *     work is enqueued on hip_stream, which belongs to the current device, and
  *     nothing is allocated, copied to the host or waited for, so every call
@@ -452,7 +452,7 @@ dex_status dex_pages_append(int32_t dtype, int32_t head_dim, const dex_rotary *r
  * A row that sees no key (row_len <= 0, a sequence outside [0, n_seqs), no
  * page) gets zeros and -inf.  No row_len exceeds max_len, which sizes the
  * work: keys past it, or past the table, are not attended to.  head_dim 32,
- * 64 or 128; n_heads a multiple of n_kv_heads, at most 64 times it; q, out and
+ * 64 or 128; n_heads a multiple of n_kv_heads, at most 64 times it and 8192; q, out and
  * the cache are of dtype, sums and statistics float.  Consecutive `group` rows
  * whose leading pages are the same (the beams of a request) have those read
  * once for all of them; any group gives the same bits.  A row's bits depend on
@@ -469,7 +469,8 @@ dex_status dex_pages_attention(int32_t dtype, int32_t head_dim, int32_t n_heads,
 /* Page tables.  ref[p] (int32 [n_pages]) counts the holders of page p: the
  * table rows that list it and any others the caller counts (a cached prefix);
  * 0 is free.  length[s] is the sequence's tokens.  Table entries behind a
- * sequence's pages are -1.  n_seqs <= 1024 here.
+ * sequence's pages are -1.  n_seqs <= 1024 and n_seqs * max_pages <= 2^30 for
+ * fork and reserve.
  *
  * dex_pages_fork: sequence s becomes a copy of sequence parent[s], sharing its
  * pages, or empty where parent[s] is not in [0, n_seqs).  Sequences that are
@@ -527,8 +528,8 @@ dex_status dex_pages_copy(int32_t dtype, int32_t head_dim, int32_t n_layers, int
  * candidates are compared by their logits, across beams in double.  logits:
  * [requests * beams][vocab] of dtype, rows ld elements apart, any alignment.
  * beams and n_out 1 .. 64, n_out <= beams * vocab, requests * beams <= 2^20,
- * requests * beams * vocab of at most 2^31 segments of 2048; eos in
- * [0, vocab), or -1 (with done NULL): none.                                  */
+ * requests * beams * (vocab / 2048 + 2) <= 2^25; eos in [0, vocab), or -1 (with
+ * done NULL): none.                                                         */
 int64_t dex_beam_select_work(int32_t dtype, int32_t requests, int32_t beams, int32_t vocab, int32_t n_out);
 dex_status dex_beam_select(int32_t dtype, const void *logits, int64_t ld, int32_t requests, int32_t beams,
                            int32_t vocab, const float *score, const uint8_t *done, int32_t eos, int32_t n_out,

@@ -54,8 +54,13 @@ const char *cache_fault(int dtype, int head_dim, int n_pages, int n_kv_heads, in
 
 const char *table_fault(int n_seqs, int max_pages, int page_size) {
   if (n_seqs < 1 || n_seqs > (1 << 24)) return "n_seqs is not 1 to 2^24";
-  if (max_pages < 1 || (int64_t)max_pages * page_size > INT32_MAX) return "max_pages is below 1, or ends past position 2^31";
+  if (max_pages < 1 || (int64_t)max_pages * page_size > (1 << 30)) return "max_pages is below 1, or ends past position 2^30";
   return nullptr;
+}
+
+// What one workgroup numbers in 32 bits: all pages that a table can list.
+const char *entries_fault(int n_seqs, int max_pages) {
+  return (int64_t)n_seqs * max_pages > (1 << 30) ? "the table has over 2^30 entries" : nullptr;
 }
 
 const char *rotary_fault(const dex_rotary *r, int head_dim) {
@@ -183,6 +188,7 @@ dex_status dex_pages_attention(int32_t dtype, int32_t head_dim, int32_t n_heads,
   REFUSE_IF(head_dim != 32 && head_dim != 64 && head_dim != 128, "head_dim is not 32, 64 or 128");
   REFUSE_IF(n_heads < n_kv_heads || n_heads % n_kv_heads || n_heads / n_kv_heads > 64,
             "n_heads is not a multiple of n_kv_heads, up to 64 times it");
+  REFUSE_IF(n_heads > 8192, "n_heads is over 8192");
   REFUSE_IF(n_rows < 0 || n_rows > (1 << 20), "n_rows is not 0 to 2^20");
   REFUSE_IF(max_len < 0 || window < 0 || group < 1, "max_len or window is below 0, or group below 1");
   REFUSE_IF(!std::isfinite(scale), "scale is not finite");
@@ -208,6 +214,7 @@ dex_status dex_pages_fork(const int32_t *table, const int32_t *ref, const int32_
   REFUSE_IF(n_seqs < 1 || n_seqs > kMaxSeqs, "n_seqs is not 1 to 1024");
   REFUSE_IF(n_pages < 1 || n_pages > (1 << 30), "n_pages is not 1 to 2^30");
   if (const char *why = table_fault(n_seqs, max_pages, 1)) return refuse(fn, why);
+  if (const char *why = entries_fault(n_seqs, max_pages)) return refuse(fn, why);
   const ForkArgs a{table, ref, length, parent, table_out, ref_out, length_out, n_seqs, max_pages, n_pages};
   return launched(fn, launch_fork(a, (hipStream_t)stream));
 }
@@ -221,6 +228,7 @@ dex_status dex_pages_reserve(int32_t *table, int32_t *ref, int32_t *length, cons
   REFUSE_IF(n_pages < 1 || n_pages > (1 << 30), "n_pages is not 1 to 2^30");
   REFUSE_IF(page_shift(page_size) < 0, "page_size is not a power of two up to 1024");
   if (const char *why = table_fault(n_seqs, max_pages, page_size)) return refuse(fn, why);
+  if (const char *why = entries_fault(n_seqs, max_pages)) return refuse(fn, why);
   const ReserveArgs a{table, ref, length, n_new, n_seqs, max_pages, n_pages, page_shift(page_size),
                       pos, src, dst, tokens, state};
   return launched(fn, launch_reserve(a, (hipStream_t)stream));
@@ -244,7 +252,7 @@ dex_status dex_pages_copy(int32_t dtype, int32_t head_dim, int32_t n_layers, int
   static const char fn[] = "dex_pages_copy";
   if (const char *why = cache_fault(dtype, head_dim, n_pages, n_kv_heads, page_size)) return refuse(fn, why);
   REFUSE_IF(head_dim * elem(dtype) % 16, "a head's row is not a multiple of 16 bytes");
-  REFUSE_IF(n_layers < 1 || n_layers > (1 << 16), "n_layers is not 1 to 2^16");
+  REFUSE_IF(n_layers < 1 || (int64_t)n_layers * n_kv_heads > (1 << 20), "n_layers is not 1 to 2^20 / n_kv_heads");
   REFUSE_IF(capacity < 0, "capacity is below 0");
   REFUSE_IF(!k_pool || !v_pool, "a pool is NULL");
   REFUSE_IF(!aligned(k_pool, 16) || !aligned(v_pool, 16), "the pools are not 16-byte aligned");
@@ -269,7 +277,7 @@ dex_status dex_beam_select(int32_t dtype, const void *logits, int64_t ld, int32_
   REFUSE_IF((int64_t)requests * beams > (1 << 20), "requests * beams is over 2^20");
   REFUSE_IF(vocab < 1 || vocab > (1 << 30), "vocab is not 1 to 2^30");
   REFUSE_IF(n_out < 1 || n_out > kMaxBeams || n_out > (int64_t)beams * vocab, "n_out is not 1 to 64, at most beams * vocab");
-  REFUSE_IF((int64_t)requests * beams * (vocab / 2048 + 2) > INT32_MAX, "too many logits for one call");
+  REFUSE_IF((int64_t)requests * beams * (vocab / 2048 + 2) > (1 << 25), "too many logits for one call");
   REFUSE_IF(eos < -1 || eos >= vocab, "eos is not in [-1, vocab)");
   REFUSE_IF(done && eos < 0, "finished beams need an eos");
   if (requests == 0) return DEX_OK;

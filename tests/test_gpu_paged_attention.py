@@ -214,3 +214,47 @@ def test_offsets_past_32_bits():
     x, x64 = normal(rng, (2, 8, hd), "bf16")              # and the write lands there too
     paged.append(k, v, ints(table), ints([311, 312]), x, x)
     assert torch.equal(v[n_pages - 1, :, 7], x[0]) and torch.equal(k[19, :, 8], x[1])
+
+
+@pytest.mark.parametrize("dtype,group", [("bf16", 1), ("bf16", 4), ("f32", 4)])
+def test_a_captured_call_follows_lengths_and_tables(dtype, group):
+    """Captured once, replayed with other lengths, other tables and other
+    queries: every replay has the bits of an eager call on them."""
+    torch = torch_cuda()
+    from paper_2606_29223_amd import paged
+    c = Case(41, dtype, 128, 8, 2, 16, [900, 900, 900, 900, 2500, 2400, 700, 0])
+    t = c.table.copy()
+    t[1, :50] = t[2, :40].tolist() + t[1, 40:50].tolist()
+    table, lens, q = ints(t), ints(c.lens), c.q.clone()
+    run = lambda: paged.attention(q, c.k, c.v, table, lens, max_len=2560, group=group, window=1500, return_lse=True)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = run()
+    for i in range(5):
+        new = c.rng.permutation(8)
+        table.copy_(ints(t[new]))
+        lens.copy_(ints(np.maximum(c.lens[new] - 37 * i, 0)))
+        q.copy_(c.q[torch.from_numpy(c.rng.permutation(8)).cuda()])
+        want = run()
+        graph.replay()
+        if i % 2:
+            torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1]), i
+
+
+def test_calls_that_overlap_on_two_streams():
+    torch = torch_cuda()
+    cases = [Case(s, "bf16", 128, 16, 4, 16, [3000, 1200, 4000, 65]) for s in (51, 52)]
+    want = [c.run() for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(6):
+        got = []
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                got.append(c.run())
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])

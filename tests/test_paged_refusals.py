@@ -69,27 +69,29 @@ BAD = (
         (dict(pos=None), "row_pos"), (dict(n_rows=-5), "n_rows"), (dict(n_rows=1 << 26), "too many")]]
     + [("dex_pages_attention", ATTENTION, *b) for b in CACHE + TABLE + [
         (dict(head_dim=96), "head_dim"), (dict(n_heads=3), "multiple"), (dict(n_heads=1), "multiple"),
-        (dict(n_heads=130), "64 times"), (dict(n_rows=-1), "n_rows"), (dict(max_len=-1), "max_len"),
+        (dict(n_heads=130), "64 times"), (dict(n_heads=8194), "64 times"), (dict(n_heads=8320, n_kv=260), "8192"), (dict(n_rows=-1), "n_rows"), (dict(max_len=-1), "max_len"),
         (dict(window=-1), "window"), (dict(group=0), "group"), (dict(scale=math.inf), "scale"), (dict(q=None), "NULL"),
         (dict(lens=None), "NULL"), (dict(out=None), "NULL"), (dict(table=None), "NULL"), (dict(work=None), "work"),
         (dict(work=FAKE + 4), "work"), (dict(k_pages=FAKE + 4), "aligned")]]
     + [("dex_pages_fork", FORK, *b) for b in TABLE + [
         (dict(n_seqs=1025), "n_seqs"), (dict(n_pages=0), "n_pages"), (dict(parent=None), "NULL"), (dict(t=None), "NULL"),
-        (dict(max_pages=-3), "max_pages")] if b[0] != dict(max_pages=1 << 28)]
+        (dict(max_pages=-3), "max_pages"), (dict(n_seqs=1024, max_pages=(1 << 20) + 1), "entries")] if b[0] != dict(max_pages=1 << 28)]
     + [("dex_pages_reserve", RESERVE, *b) for b in TABLE + [
         (dict(n_seqs=1025), "n_seqs"), (dict(n_pages=(1 << 30) + 1), "n_pages"), (dict(page_size=3), "power of two"),
-        (dict(n_new=None), "NULL"), (dict(state=None), "NULL"), (dict(tokens=None), "NULL")]]
+        (dict(n_new=None), "NULL"), (dict(state=None), "NULL"), (dict(tokens=None), "NULL"),
+        (dict(n_seqs=1024, max_pages=(1 << 20) + 1, page_size=8), "entries")]]
     + [("dex_pages_compact", COMPACT, *b) for b in [
         (dict(n_pages=0), "n_pages"), (dict(src=None), "NULL"), (dict(map=None), "NULL"), (dict(n_seqs=0), "n_seqs"),
         (dict(max_pages=0), "max_pages")]]
     + [("dex_pages_copy", COPY, *b) for b in CACHE + [
-        (dict(head_dim=4), "16 bytes"), (dict(n_layers=0), "n_layers"), (dict(capacity=-1), "capacity"),
+        (dict(head_dim=4), "16 bytes"), (dict(n_layers=0), "n_layers"),
+        (dict(n_layers=(1 << 19) + 1), "n_layers"), (dict(capacity=-1), "capacity"),
         (dict(k=None), "NULL"), (dict(src=None), "NULL"), (dict(v=FAKE + 8), "aligned")]]
     + [("dex_beam_select", BEAM, *b) for b in [
         (dict(dtype=-1), "dtype"), (dict(beams=0), "beams"), (dict(beams=65), "beams"), (dict(n_out=0), "n_out"),
         (dict(n_out=65), "n_out"), (dict(vocab=0), "vocab"), (dict(vocab=1, n_out=5), "n_out"), (dict(eos=500), "eos"),
         (dict(eos=-2), "eos"), (dict(done=FAKE), "eos"), (dict(ld=499), "ld"), (dict(requests=-1), "requests"),
-        (dict(requests=1 << 19), "2^20"), (dict(requests=1 << 18, beams=4, vocab=1 << 26, ld=1 << 26), "too many"),
+        (dict(requests=1 << 19), "2^20"), (dict(requests=1 << 17, beams=8, vocab=1 << 17, ld=1 << 17), "too many"),
         (dict(score=None), "NULL"), (dict(work=None), "NULL"), (dict(work=FAKE + 8), "aligned"),
         (dict(logits=FAKE + 1), "aligned")]]
 )
