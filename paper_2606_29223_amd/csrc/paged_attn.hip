@@ -457,6 +457,9 @@ __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2
                                                                  float2 *stat) {
   using W = Wave<T, HD, NB, RUN>;
   constexpr int UNIT_TILES = PA_UNIT / W::TK;
+  // (the LDS below is at most half of a compute unit's 160 KiB, 80.4 KB at
+  // head_dim 128 in bf16; with 82.5 KB one workgroup a unit was left and 8 x
+  // 8300 keys took 77 us for 62)
   __shared__ Lds<T, HD> lds_all[PA_WAVES];
   __shared__ int first_item[PA_ROWS], keys_of[PA_ROWS], share_of[PA_ROWS];   // items before a row's; its keys
   __shared__ int part[PA_WAVES];
@@ -758,9 +761,11 @@ hipError_t go(const PagedAttnArgs &a, int rows_along, hipStream_t s) {
       if (e != hipSuccess) return e;
       g.share = share;
     }
-    // two workgroups fit a compute unit; further items wait their turn in them
+    // the workgroups that fit a compute unit, by their registers; further items
+    // wait their turn in them (two a unit everywhere: 2 to 6 % slower below 128)
+    constexpr int kPerUnit = HD * NB > 64 ? 2 : HD * NB == 64 ? 3 : 4;
     paged_attn_kernel<T, HD, NB, RUN>
-        <<<(unsigned)std::min<int64_t>(row_items * smax, 512), PA_THREADS, 0, s>>>(b, g, smax, rec, stat);
+        <<<(unsigned)std::min<int64_t>(row_items * smax, 256 * kPerUnit), PA_THREADS, 0, s>>>(b, g, smax, rec, stat);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (smax > 1) {

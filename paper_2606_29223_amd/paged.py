@@ -73,10 +73,22 @@ def _heads(t, device, dtype, shape, name):
     if t.dtype is not dtype or t.device != device or t.shape != shape:
         _refuse(f"{name}: {dtype} of shape {tuple(shape)} on {device} is wanted, "
                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    s = t.stride()
-    if s[2] != 1 and shape[2] > 1:
+    return _strided(t, name)
+
+
+def _strided(t, name):
+    r, h, d = t.stride()
+    if d != 1 and t.shape[2] > 1:
         _refuse(f"{name}: head_dim has to be dense")
-    return t.data_ptr(), s[0], s[1]
+    return t.data_ptr(), r, h
+
+
+def _out(t, like, shape, name):
+    """The caller's output, checked, or a new one: (tensor, address and strides)."""
+    if t is not None:
+        return t, _heads(t, like.device, like.dtype, shape, name)
+    t = like.new_empty(shape)
+    return t, (t.data_ptr(), shape[1] * shape[2], shape[2])
 
 
 def _gpu(t, name):
@@ -122,7 +134,7 @@ class Rotary:
         lib = dexlib.load()
         dexlib._check(lib, None, lib.dex_rotary_turns(SCALING[scaling], self.rot_dim, theta, factor, original, slow, fast,
                                                       turns))
-        self.turns = torch.tensor(list(turns), dtype=torch.float64, device=device)
+        self.turns = torch.frombuffer(turns, dtype=torch.float64).to(device, copy=True)
         self.struct = dexlib.DexRotary(self.turns.data_ptr(), self.rot_dim, int(bool(interleaved)), float(amplitude))
 
 
@@ -142,17 +154,13 @@ def rope(rotary, pos, q, k=None, q_out=None, k_out=None, inverse=False):
         _refuse("queries and keys are [rows, heads, head_dim]")
     rows, heads, hd = q.shape
     plan = _plan(rotary, dev, hd)
-    if q_out is None:
-        q_out = torch.empty((rows, heads, hd), dtype=dt, device=dev)
-    a = _heads(q, dev, dt, q.shape, "q")
-    b = _heads(q_out, dev, dt, q.shape, "q_out")
+    a = _strided(q, "q")
+    q_out, b = _out(q_out, q, (rows, heads, hd), "q_out")
     n, c, o = 0, (None, 0, 0), (None, 0, 0)
     if k is not None:
         n = k.shape[1]
-        if k_out is None:
-            k_out = torch.empty((rows, n, hd), dtype=dt, device=dev)
         c = _heads(k, dev, dt, (rows, n, hd), "k")
-        o = _heads(k_out, dev, dt, (rows, n, hd), "k_out")
+        k_out, o = _out(k_out, q, (rows, n, hd), "k_out")
     p = _ints(pos, dev, (rows,), "pos")
     if rows > 0:
         _run(dexlib.load().dex_rope, dev, d, hd, plan, inverse, rows, p, *a, heads, *b, *c, n, *o)
@@ -175,9 +183,7 @@ def append(k_pages, v_pages, table, pos, k, v, seq=None, rotary=None, q=None, q_
         heads = q.shape[1]
         qs = (rows, heads, hd)
         a = _heads(q, dev, dt, qs, "q")
-        if q_out is None:
-            q_out = torch.empty(qs, dtype=dt, device=dev)
-        o = _heads(q_out, dev, dt, qs, "q_out")
+        q_out, o = _out(q_out, q, qs, "q_out")
     b, c = _heads(k, dev, dt, shape, "k"), _heads(v, dev, dt, shape, "v")
     ts = table.shape
     tab = _ints(table, dev, ts, "table")
@@ -204,9 +210,8 @@ def attention(q, k_pages, v_pages, table, lens, seq=None, max_len=None, scale=No
         _refuse("queries are [rows, heads, head_dim]")
     rows, heads = q.shape[0], q.shape[1]
     shape = (rows, heads, hd)
-    if out is None:
-        out = torch.empty(shape, dtype=dt, device=dev)
-    a, o = _heads(q, dev, dt, shape, "q"), _heads(out, dev, dt, shape, "out")
+    a = _heads(q, dev, dt, shape, "q")
+    out, o = _out(out, q, shape, "out")
     ts = table.shape
     tab = _ints(table, dev, ts, "table")
     n = _ints(lens, dev, (rows,), "lens")
@@ -349,9 +354,9 @@ def beam_select(logits, scores, n_out=None, done=None, eos=-1):
     if n < 1:
         _refuse("n_out is below 1")
     shape = (requests, n)
-    parent, token = (torch.empty(shape, dtype=torch.int32, device=dev) for _ in range(2))
-    score = torch.empty(shape, dtype=torch.float32, device=dev)
-    ends = torch.empty(shape, dtype=torch.bool, device=dev)
+    score = torch.empty_like(scores) if n == beams else scores.new_empty(shape)
+    parent = torch.empty_like(score, dtype=torch.int32)
+    token, ends = torch.empty_like(parent), torch.empty_like(score, dtype=torch.bool)
     if requests > 0:
         lib = dexlib.load()
         work = torch.empty(max(16, lib.dex_beam_select_work(d, requests, beams, vocab, n)), dtype=torch.uint8, device=dev)
