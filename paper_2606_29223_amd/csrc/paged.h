@@ -56,7 +56,7 @@ struct RopeArgs {
   PageMap map;
   const int *seq;             // [n_rows], or null: row r is sequence r
 };
-// vec: pairs a lane turns at a time (rope_vec)
+// Pairs a lane turns at a time: the widest access that the call allows.
 int rope_vec(int dtype, const RopeArgs &a);
 hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t s);
 

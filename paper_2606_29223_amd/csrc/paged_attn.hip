@@ -18,6 +18,13 @@
 // kernel; the products are 4 % of what the matrix cores could do meanwhile.
 // That is why P goes through them in two bf16 parts (p = hi + lo to 2^-17): it
 // costs the output no accuracy and no time.
+//
+// Measured (32 / 8 heads of 128, bf16): 8 rows of 8300 keys 56.8 us and the join
+// 4.7 for 272 MB, 4.8 TB/s in the kernel; 64 rows of 1 to 16000 keys 99 + 4.9
+// (461 MB); the loads alone, without products, take as long (392 of 399 us at 64
+// x 8000).  A single short row is the latency of the chain length, table, keys,
+// products, join: 9.2 + 3.3 us at 700 keys.  Splits: with 32 a row the records
+// cost 64 x 8000 keys 5 %, with 16 one long row lost 8 %.
 #include "attn_decode.h"
 #include "dex.h"
 #include "paged.h"
@@ -397,7 +404,8 @@ __device__ __forceinline__ int group_rows(const Sharing &g, int r, int n_rows) {
 }
 
 // The leading splits that are the same keys for every row of a group: one
-// workgroup compares their table rows.  They are the same work only where all
+// workgroup compares their table rows (6 us; 16 x 8 rows that share 4000 of 4090
+// keys then take 85 + 9 us, alone 261 + 32).  They are the same work only where all
 // rows are cut alike and see all of the split, or all have one length.
 __global__ __launch_bounds__(PA_THREADS) void paged_share_kernel(PagedAttnArgs a, Sharing g, int *share) {
   __shared__ int lens[PA_COLS], seqs[PA_COLS], first;

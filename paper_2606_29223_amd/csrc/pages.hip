@@ -1,6 +1,11 @@
 // Page tables of a paged cache: fork and free, reserve with copy on write,
 // compaction, and the copies of pages they ask for.
 //
+// Tables are small: all of a step's kernels but the copy are bound by the
+// latency of a few dependent loads, so they take few launches and ask for
+// everything they can at once.  64 rows of 58 pages: fork 2.9 us, reserve 5.9;
+// compaction of 4096 pages 7.5 and its table 4.6.
+//
 // A table row holds a sequence's pages in order, then -1.  ref[p] counts the
 // rows (and whoever else) that hold page p; a page nobody holds has count 0
 // and may be taken.  Everything is decided on the device, in one fixed order
@@ -444,7 +449,9 @@ hipError_t launch_compact(const CompactArgs &a, hipStream_t s) {
 // Entry i of the list: the first tokens[i] slots (all, without tokens) of
 // page src[i] of every layer, key and value and head go to page dst[i].  A
 // workgroup takes about 16 KiB of one page at a time: heads of one layer's
-// keys or values.
+// keys or values, four 16-byte loads a lane on their way.  Bound by memory: 40
+// part pages of 32 layers (70 MB read and written) 14 us, 5.0 TB/s; 1000 pages
+// of 12 layers (1.18 GB) 246 us, 4.8 TB/s, as a large copy.
 __global__ __launch_bounds__(256) void page_copy_kernel(PageCopyArgs a, int heads, int parts) {
   const int count = min(a.count != nullptr ? *a.count : a.capacity, a.capacity);
   const int part = blockIdx.x % parts, kv = blockIdx.x / parts & 1, layer = blockIdx.x / parts >> 1;

@@ -70,7 +70,11 @@ struct Vec {
 
 // A lane owns one unit of a row -- VEC pairs, or 2 VEC elements past rot_dim --
 // works out its VEC angles once and takes the unit through the heads
-// slot, slot + slots, ... of queries, keys and values.
+// slot, slot + slots, ... of queries, keys and values.  With the angles shared
+// memory bounds the kernel: 8192 rows of 32 and 8 heads of 128 in
+// bf16 (168 MB) take 33 us, with the values written to pages too (201 MB) 41 us,
+// 5.0 TB/s, where a copy of that size runs at 5.3.  A few rows take 3.5 to 4.5
+// us, the launch and two dependent loads.
 template <typename T, int VEC, bool INTER>
 __global__ __launch_bounds__(ROPE_THREADS) void rope_kernel(RopeArgs a, int units, int slots) {
   const int tid = blockIdx.x * ROPE_THREADS + threadIdx.x;
@@ -176,10 +180,14 @@ int rope_vec(int dtype, const RopeArgs &a) {
 template <typename T, int VEC>
 static hipError_t rope_go(const RopeArgs &a, hipStream_t s) {
   const int units = a.head_dim / (2 * VEC), jobs = a.q.n + a.k.n + a.v.n;
-  // heads a lane: one while that leaves fewer than 2^17 lanes (two waves a
-  // SIMD), then up to eight, which share one set of angles
+  // Heads a lane: one while that leaves fewer than 2^18 lanes (500 rows of 40
+  // heads of 128 in bf16: 5.5 us with one, 8.7 with eight), then more, which
+  // share one set of angles, up to eight in bf16 (8192 rows written to pages: 55
+  // us with one, 40 with eight) and four in fp32, where the angles weigh half as
+  // much (8192 rows: 62 with one, 64 with four, 67 with eight).
+  const int most = sizeof(T) == 2 ? 8 : 4;
   int heads = 1;
-  while (heads < 8 && (int64_t)a.n_rows * units * ((jobs + heads - 1) / heads) > (1 << 17)) heads *= 2;
+  while (heads < most && (int64_t)a.n_rows * units * ((jobs + heads - 1) / heads) > (1 << 18)) heads *= 2;
   const int slots = (jobs + heads - 1) / heads;
   const int64_t lanes = (int64_t)a.n_rows * units * slots;
   const dim3 grid((unsigned)((lanes + ROPE_THREADS - 1) / ROPE_THREADS));
