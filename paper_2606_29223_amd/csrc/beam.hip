@@ -382,9 +382,15 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void beam_join_kernel(BeamArgs a, 
 
 }  // namespace
 
-// Logits of a lane: 32, or 8 where segments of 2048 would leave most of the
-// GPU's 1024 SIMDs without a wave and a call is one wave's time.
-static int lane_logits(int rows, int vocab) { return (int64_t)rows * segments(vocab, 8, 2048) < 512 ? 8 : 32; }
+// Logits of a lane: 32, or 8 where that leaves the join of a row one segment a
+// lane and the GPU's 1024 SIMDs at most a wave each, so that a call is one wave's
+// time. 8 against 32, bf16, us: 4 rows of 8000 logits 9.2 / 10.5, of 32000 9.5 /
+// 10.2, 16 rows of 32000 13.1 / 13.5; past either limit 8 rows of 65000 16.7 /
+// 13.6, 64 rows of 32000 14.4 / 13.9, 512 rows 30.3 / 23.0.
+static int lane_logits(int rows, int vocab) {
+  const int n_seg = segments(vocab, 8, 64 * 8);
+  return n_seg <= 64 && (int64_t)rows * n_seg <= 1024 ? 8 : 32;
+}
 
 size_t beam_work(int dtype, int rows, int vocab, int n_out) {
   const size_t n_seg = segments(vocab, dtype == DEX_F32 ? kGrain<float> : kGrain<uint16_t>, 64 * lane_logits(rows, vocab));
