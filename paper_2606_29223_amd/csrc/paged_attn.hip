@@ -739,7 +739,7 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedAttnArgs a,
   finish<T, RUN>(a, row, head, 4 * d, o, m, l);
 }
 
-int max_splits(int max_len) { return std::max(1, std::min(PA_SPLITS, (max_len + kSplitKeys - 1) / kSplitKeys)); }
+int max_splits(int max_len) { return max_len > 0 ? std::min(PA_SPLITS, (max_len - 1) / kSplitKeys + 1) : 1; }
 
 // The call's rows in launches of at most PA_ROWS.
 template <typename T, int HD, int NB, int RUN>

@@ -122,6 +122,14 @@ def test_work_sizes(lib):
     assert lib.dex_beam_select_work(7, 2, 4, 500, 4) == 0
 
 
+def test_the_largest_max_len_needs_the_work_of_a_long_one(lib):
+    need = lib.dex_pages_attention_work(4, 32, 8, 128, 1 << 30, 1)
+    for n in (2 ** 31 - 1, 2 ** 31 - 200, 1 << 20):
+        assert lib.dex_pages_attention_work(4, 32, 8, 128, n, 1) == need
+        assert _call(lib, "dex_pages_attention", ATTENTION, max_len=n, work=None) == dexlib.DEX_E_INVAL
+    assert "work" in lib.dex_last_error(None).decode()
+
+
 SCALINGS = [dict(scaling=None), dict(scaling="linear", factor=4.0), dict(scaling="base", factor=8.0),
             dict(scaling="bands", factor=16.0, original=8192.0, slow=1.0, fast=32.0)]
 
