@@ -184,12 +184,14 @@ static hipError_t rope_go(const RopeArgs &a, hipStream_t s) {
   // heads of 128 in bf16: 5.5 us with one, 8.7 with eight), then more, which
   // share one set of angles, up to eight in bf16 (8192 rows written to pages: 55
   // us with one, 40 with eight) and four in fp32, where the angles weigh half as
-  // much (8192 rows: 62 with one, 64 with four, 67 with eight).
+  // much (8192 rows: 62 with one, 64 with four, 67 with eight).  The limit on a
+  // call's elements is for eight: fewer may leave more lanes than an int counts.
   const int most = sizeof(T) == 2 ? 8 : 4;
   int heads = 1;
-  while (heads < most && (int64_t)a.n_rows * units * ((jobs + heads - 1) / heads) > (1 << 18)) heads *= 2;
+  auto lanes_of = [&](int h) { return (int64_t)a.n_rows * units * ((jobs + h - 1) / h); };
+  while (heads < 8 && lanes_of(heads) > (heads < most ? 1 << 18 : 1 << 30)) heads *= 2;
   const int slots = (jobs + heads - 1) / heads;
-  const int64_t lanes = (int64_t)a.n_rows * units * slots;
+  const int64_t lanes = lanes_of(heads);
   const dim3 grid((unsigned)((lanes + ROPE_THREADS - 1) / ROPE_THREADS));
   if (a.interleaved) rope_kernel<T, VEC, true><<<grid, ROPE_THREADS, 0, s>>>(a, units, slots);
   else rope_kernel<T, VEC, false><<<grid, ROPE_THREADS, 0, s>>>(a, units, slots);

@@ -81,6 +81,25 @@ def test_strides_alignment_and_in_place_have_the_same_bits(dtype):
     assert torch.equal(x[:, :h], want_q) and torch.equal(x[:, h:h + kv], want_k)
 
 
+def test_as_many_rows_as_a_call_takes():
+    """1.3 billion rows of five fp32 heads of one pair (52 GB), close to the
+    limit of a call: more lanes of four heads than an int counts."""
+    torch = torch_cuda()
+    from paper_2606_29223_amd import paged
+    rows = 1_300_000_000
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("less than 80 GiB of GPU memory is free")
+    plan = paged.Rotary(2)
+    x, _ = normal(np.random.default_rng(8), (1, 5, 2), "f32")
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda")
+    got = paged.rope(plan, pos, x.expand(rows, 5, 2))
+    some = torch.randint(0, rows, (100_000,), generator=torch.Generator().manual_seed(1)).cuda()
+    some[:2] = torch.tensor([0, rows - 1])
+    assert torch.equal(got[some], paged.rope(plan, pos[some], x.expand(len(some), 5, 2)))
+    del got, pos
+    torch.cuda.empty_cache()
+
+
 def test_a_turn_back_is_the_gradient():
     """The gradient of sum(g * rope(x)) by differences, which a linear map's
     are exact to rounding: each difference of sums is off by rows * heads * hd
