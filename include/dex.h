@@ -380,10 +380,13 @@ dex_status dex_debug_copy(void *dst, const void *src, int64_t bytes, void *hip_s
  *     nothing is allocated, copied to the host or waited for, so every call
  *     can be captured into a graph.  What a call reads on the device (lengths,
  *     tables, parents) may change between replays; its sizes may not.
+ *   - Arrays are aligned to their type.  Elements of a strided output do not
+ *     overlap each other, and an output overlaps no input unless the call says
+ *     that it may.
  *   - Work memory is the caller's: the size that the matching _work function
- *     gives (0: may be NULL), 16-byte aligned, with any contents.  It is free for another use
- *     once the call's work is done; two calls that may overlap in time (two
- *     streams, two graphs) need one each.
+ *     gives (0: may be NULL), 16-byte aligned, with any contents.  It is free
+ *     for another use once the call's work is done; two calls that may overlap
+ *     in time (two streams, two graphs) need one each.
  *   - Argument errors return DEX_E_INVAL before anything is launched, with
  *     the reason in dex_last_error(NULL).  Numbers on the device cannot be
  *     refused; each call says what it makes of those that do not fit, and
@@ -492,7 +495,7 @@ dex_status dex_pages_fork(const int32_t *table, const int32_t *ref, const int32_
  *   pos[s]     the first new position, or -1 (nothing asked, or not granted);
  *   src, dst, tokens     int32 [n_seqs], the copies first, then -1, -1, 0;
  *   state      int32 [4]: copies, pages taken, pages missing, 1 if a sequence
- *              outgrows the table or has a length below 0.
+ *              that asks for tokens outgrows the table or has a length below 0.
  * Unless state[2] and state[3] are 0 nothing was granted: table, ref and length
  * stay, every pos is -1 and the list is empty.                              */
 dex_status dex_pages_reserve(int32_t *table, int32_t *ref, int32_t *length, const int32_t *n_new, int32_t n_seqs,

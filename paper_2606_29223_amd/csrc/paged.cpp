@@ -34,6 +34,25 @@ bool known(int dtype) { return dtype == DEX_F32 || dtype == DEX_BF16; }
 int64_t elem(int dtype) { return dtype == DEX_F32 ? 4 : 2; }
 bool aligned(const void *p, uintptr_t to) { return (uintptr_t)p % to == 0; }
 
+// Arrays of int32 (or float) at their type's alignment: counts change by atomics.
+template <typename... P>
+bool words(P... p) {
+  return (aligned(p, 4) && ...);
+}
+
+// Whether elements of an output share memory.  A row's heads lie apart from each
+// other and the rows apart from each other, or the other way round.
+bool overlaps(int64_t n_rows, int64_t row, int64_t heads, int64_t head, int64_t head_dim) {
+  typedef __int128 wide;
+  const wide r = row < 0 ? -(wide)row : row, h = head < 0 ? -(wide)head : head;
+  auto apart = [&](wide n0, wide s0, wide n1, wide s1) {      // n0 inside n1
+    return (n0 == 1 || s0 >= head_dim) && (n1 == 1 || s1 >= (n0 - 1) * s0 + head_dim);
+  };
+  return n_rows > 0 && heads > 0 && !apart(heads, h, n_rows, r) && !apart(n_rows, r, heads, h);
+}
+const char kOverlap[] = "elements of an output overlap";
+const char kType[] = "an array is not aligned to its type";
+
 // log2 of a page size, -1 if it is none
 int page_shift(int page_size) {
   if (page_size < 1 || page_size > 1024 || (page_size & (page_size - 1))) return -1;
@@ -65,6 +84,7 @@ const char *entries_fault(int n_seqs, int max_pages) {
 
 const char *rotary_fault(const dex_rotary *r, int head_dim) {
   if (!r->turns) return "the plan has no turns";
+  if (!aligned(r->turns, 8)) return "the plan's turns are not aligned to their type";
   if (r->rot_dim < 2 || r->rot_dim % 2 || r->rot_dim > head_dim) return "rot_dim is not even, 2 to head_dim";
   if (!std::isfinite(r->amplitude)) return "amplitude is not finite";
   return nullptr;
@@ -106,6 +126,7 @@ dex_status dex_rotary_turns(int32_t scaling, int32_t rot_dim, double theta, doub
       const double keep = std::fmin(1.0, std::fmax(0.0, (n - slow) / (fast - slow)));
       f = f * keep + f / factor * (1.0 - keep);
     }
+    if (!std::isfinite(f)) return refuse(fn, "theta and factor give a frequency that is not finite");
     turns[i] = f / two_pi;
   }
   return DEX_OK;
@@ -125,6 +146,10 @@ dex_status dex_rope(int32_t dtype, int32_t head_dim, const dex_rotary *rotary, i
   REFUSE_IF(n_heads + n_kv_heads == 0, "neither queries nor keys");
   REFUSE_IF((n_heads > 0 && !q_out) || (n_kv_heads > 0 && !k_out), "an output is NULL");
   REFUSE_IF(n_rows < 0 || (n_rows > 0 && !pos), "n_rows is below 0, or pos is NULL");
+  REFUSE_IF(!words(pos) || !aligned(q, elem(dtype)) || !aligned(q_out, elem(dtype)) || !aligned(k, elem(dtype)) ||
+                !aligned(k_out, elem(dtype)), kType);
+  REFUSE_IF(overlaps(n_rows, q_out_row, n_heads, q_out_head, head_dim) ||
+                overlaps(n_rows, k_out_row, n_kv_heads, k_out_head, head_dim), kOverlap);
   REFUSE_IF(too_many(n_rows, head_dim, n_heads + n_kv_heads), "too many rows for one call");
   if (n_rows == 0) return DEX_OK;
   RopeArgs a{};
@@ -153,6 +178,9 @@ dex_status dex_pages_append(int32_t dtype, int32_t head_dim, const dex_rotary *r
   REFUSE_IF(!k || !v || !k_pages || !v_pages || !table, "keys, values, pages or table are NULL");
   REFUSE_IF(!aligned(k_pages, 16) || !aligned(v_pages, 16), "the pages are not 16-byte aligned");
   REFUSE_IF(n_rows < 0 || (n_rows > 0 && !row_pos), "n_rows is below 0, or row_pos is NULL");
+  REFUSE_IF(!words(row_seq, row_pos, table) || !aligned(q, elem(dtype)) || !aligned(q_out, elem(dtype)) ||
+                !aligned(k, elem(dtype)) || !aligned(v, elem(dtype)), kType);
+  REFUSE_IF(overlaps(n_rows, q_out_row, n_heads, q_out_head, head_dim), kOverlap);
   REFUSE_IF(too_many(n_rows, head_dim, n_heads + 2 * n_kv_heads), "too many rows for one call");
   if (n_rows == 0) return DEX_OK;
   RopeArgs a{};
@@ -195,6 +223,8 @@ dex_status dex_pages_attention(int32_t dtype, int32_t head_dim, int32_t n_heads,
   if (n_rows == 0) return DEX_OK;
   REFUSE_IF(!q || !k_pages || !v_pages || !table || !row_len || !out, "queries, pages, table, lengths or out are NULL");
   REFUSE_IF(!aligned(k_pages, 16) || !aligned(v_pages, 16), "the pages are not 16-byte aligned");
+  REFUSE_IF(!words(row_seq, row_len, table, lse) || !aligned(q, elem(dtype)) || !aligned(out, elem(dtype)), kType);
+  REFUSE_IF(overlaps(n_rows, out_row, n_heads, out_head, head_dim), kOverlap);
   PagedAttnArgs a{};
   a.q = q; a.q_row = q_row; a.q_head = q_head; a.k = k_pages; a.v = v_pages;
   a.map = PageMap{table, n_seqs, max_pages, n_pages, n_kv_heads, page_shift(page_size)};
@@ -215,6 +245,7 @@ dex_status dex_pages_fork(const int32_t *table, const int32_t *ref, const int32_
   REFUSE_IF(n_pages < 1 || n_pages > (1 << 30), "n_pages is not 1 to 2^30");
   if (const char *why = table_fault(n_seqs, max_pages, 1)) return refuse(fn, why);
   if (const char *why = entries_fault(n_seqs, max_pages)) return refuse(fn, why);
+  REFUSE_IF(!words(table, ref, length, parent, table_out, ref_out, length_out), kType);
   const ForkArgs a{table, ref, length, parent, table_out, ref_out, length_out, n_seqs, max_pages, n_pages};
   return launched(fn, launch_fork(a, (hipStream_t)stream));
 }
@@ -229,6 +260,7 @@ dex_status dex_pages_reserve(int32_t *table, int32_t *ref, int32_t *length, cons
   REFUSE_IF(page_shift(page_size) < 0, "page_size is not a power of two up to 1024");
   if (const char *why = table_fault(n_seqs, max_pages, page_size)) return refuse(fn, why);
   if (const char *why = entries_fault(n_seqs, max_pages)) return refuse(fn, why);
+  REFUSE_IF(!words(table, ref, length, n_new, pos, src, dst, tokens, state), kType);
   const ReserveArgs a{table, ref, length, n_new, n_seqs, max_pages, n_pages, page_shift(page_size),
                       pos, src, dst, tokens, state};
   return launched(fn, launch_reserve(a, (hipStream_t)stream));
@@ -242,6 +274,7 @@ dex_status dex_pages_compact(const int32_t *table, const int32_t *ref, int32_t n
   REFUSE_IF(n_pages < 1 || n_pages > (1 << 30), "n_pages is not 1 to 2^30");
   REFUSE_IF(n_pages > 1 && (!src || !dst), "src or dst is NULL");
   if (const char *why = table_fault(n_seqs, max_pages, 1)) return refuse(fn, why);
+  REFUSE_IF(!words(table, ref, table_out, ref_out, map, src, dst, state), kType);
   const CompactArgs a{table, ref, table_out, ref_out, map, src, dst, state, n_seqs, max_pages, n_pages};
   return launched(fn, launch_compact(a, (hipStream_t)stream));
 }
@@ -258,13 +291,15 @@ dex_status dex_pages_copy(int32_t dtype, int32_t head_dim, int32_t n_layers, int
   REFUSE_IF(!aligned(k_pool, 16) || !aligned(v_pool, 16), "the pools are not 16-byte aligned");
   if (capacity == 0) return DEX_OK;
   REFUSE_IF(!src || !dst, "src or dst is NULL");
+  REFUSE_IF(!words(src, dst, tokens, count), kType);
   const PageCopyArgs a{k_pool, v_pool, n_layers, n_pages, n_kv_heads, page_size, (int)(head_dim * elem(dtype)),
                        src, dst, tokens, count, capacity};
   return launched(fn, launch_page_copy(a, (hipStream_t)stream));
 }
 
 int64_t dex_beam_select_work(int32_t dtype, int32_t requests, int32_t beams, int32_t vocab, int32_t n_out) {
-  if (!known(dtype) || requests < 0 || beams < 1 || vocab < 1 || n_out < 1) return 0;
+  if (!known(dtype) || requests < 0 || beams < 1 || vocab < 1 || n_out < 1 || n_out > kMaxBeams) return 0;
+  if ((int64_t)requests * beams > (1 << 20)) return 0;
   return (int64_t)beam_work(dtype, (int64_t)requests * beams, vocab, n_out);
 }
 
@@ -284,7 +319,7 @@ dex_status dex_beam_select(int32_t dtype, const void *logits, int64_t ld, int32_
   REFUSE_IF(ld < vocab && (int64_t)requests * beams > 1, "ld is below vocab");
   REFUSE_IF(!logits || !score || !parent || !token || !score_out || !work, "an array is NULL");
   REFUSE_IF(!aligned(work, 16), "the work memory is not 16-byte aligned");
-  REFUSE_IF(!aligned(logits, elem(dtype)), "the logits are not aligned to their type");
+  REFUSE_IF(!aligned(logits, elem(dtype)) || !words(score, parent, token, score_out), kType);
   BeamArgs a{};
   a.logits = logits; a.ld = ld; a.requests = requests; a.beams = beams; a.vocab = vocab; a.n_out = n_out;
   a.score = score; a.done = done; a.eos = eos; a.parent = parent; a.token = token; a.score_out = score_out;

@@ -10,8 +10,10 @@ sequences' tokens (int32).  `PagedCache` holds them together.
 
 Every function enqueues on the tensors' device, on the stream that is current
 there, and waits for nothing: calls can be captured into a graph.  Outputs and
-work memory come from torch's allocator, call by call.  Bad arguments raise
-`DexError` before anything is launched.
+work memory come from torch's allocator, call by call; an output of the
+caller's overlaps no input unless the function says that it may.  Bad arguments
+raise `DexError` before anything is launched.  Nothing is recorded for
+autograd.
 
 A step of a decoding loop with branches, for a model of the caller's:
 
@@ -146,8 +148,8 @@ def _plan(rotary, device, head_dim):
 
 def rope(rotary, pos, q, k=None, q_out=None, k_out=None, inverse=False):
     """Queries (and keys) [rows, heads, head_dim] turned to positions `pos`
-    [rows] int32; `inverse` turns back (the gradient of the turn).  Returns
-    q_out, or (q_out, k_out)."""
+    [rows] int32; `inverse` turns back (the gradient of the turn).  An output
+    may be its input.  Returns q_out, or (q_out, k_out)."""
     d = _gpu(q, "q")
     dev, dt = q.device, q.dtype
     if q.dim() != 3 or (k is not None and k.dim() != 3):
@@ -163,7 +165,7 @@ def rope(rotary, pos, q, k=None, q_out=None, k_out=None, inverse=False):
         k_out, o = _out(k_out, q, (rows, n, hd), "k_out")
     p = _ints(pos, dev, (rows,), "pos")
     if rows > 0:
-        _run(dexlib.load().dex_rope, dev, d, hd, plan, inverse, rows, p, *a, heads, *b, *c, n, *o)
+        _run(dexlib.load().dex_rope, dev, d, hd, plan, 1 if inverse else 0, rows, p, *a, heads, *b, *c, n, *o)
     return q_out if k is None else (q_out, k_out)
 
 
@@ -219,6 +221,8 @@ def attention(q, k_pages, v_pages, table, lens, seq=None, max_len=None, scale=No
     most = ts[1] * ps
     if max_len is None or max_len > most:
         max_len = most
+    if max_len < 0 or not 0 <= window < 1 << 31 or not 1 <= group < 1 << 31:
+        _refuse("max_len or window is below 0, or group below 1, or past 2^31 - 1")
     lse = torch.empty((rows, heads), dtype=torch.float32, device=dev) if return_lse else None
     if rows > 0:
         lib = dexlib.load()
@@ -274,6 +278,8 @@ def reserve(table, ref, lens, n_new, page_size):
     and lens, with copies on write where a partly filled page is shared.  If
     the pages do not suffice nothing changes and every pos is -1."""
     dev, p = _tables(table, ref, lens)
+    if not 1 <= page_size <= 1024:
+        _refuse("page_size is not a power of two up to 1024")
     n, c = table.shape
     pn = _ints(n_new, dev, (n,), "n_new")
     buf = torch.empty(4 * n + 4, dtype=torch.int32, device=dev)
@@ -351,8 +357,8 @@ def beam_select(logits, scores, n_out=None, done=None, eos=-1):
                              or not done.is_contiguous()):
         _refuse("done is a contiguous bool tensor like scores")
     n = beams if n_out is None else int(n_out)
-    if n < 1:
-        _refuse("n_out is below 1")
+    if not 1 <= n <= 64 or not -1 <= eos < vocab:
+        _refuse("n_out is not 1 to 64, or eos not in [-1, vocab)")
     shape = (requests, n)
     score = torch.empty_like(scores) if n == beams else scores.new_empty(shape)
     parent = torch.empty_like(score, dtype=torch.int32)

@@ -182,3 +182,26 @@ def test_a_full_cache_grants_nothing():
     c.fork(ints([0, 1, 2, -1, -1, -1]))
     got = c.reserve(ints([1, 1, 1, 0, 0, 0]))
     assert host(got.state).tolist() == [0, 3, 0, 0] and host(got.pos).tolist() == [4, 4, 4, -1, -1, -1]
+
+
+def test_the_binding_refuses_numbers_and_outputs_that_do_not_fit():
+    torch = torch_cuda()
+    from paper_2606_29223_amd import paged
+    from paper_2606_29223_amd.dexlib import DEX_E_INVAL, DexError
+    cache = paged.PagedCache(1, 2, 32, 8, 6, 3, 4)
+    x, pos = torch.zeros((3, 2, 32), dtype=torch.bfloat16, device="cuda"), torch.zeros_like(cache.lens)
+    one = torch.zeros((1, 2, 32), dtype=torch.bfloat16, device="cuda").expand(3, 2, 32)
+    plan = paged.Rotary(32)
+    logits, score = torch.zeros((6, 50), device="cuda"), torch.zeros((3, 2), device="cuda")
+    for call in (lambda: paged.rope(plan, pos, x, q_out=one), lambda: cache.attention(0, x, out=one),
+                 lambda: cache.attention(0, x, group=2 ** 32 + 1), lambda: cache.attention(0, x, window=2 ** 32),
+                 lambda: cache.attention(0, x, max_len=-(2 ** 32)), lambda: cache.append(0, pos, x[:2], x, x),
+                 lambda: paged.reserve(cache.table, cache.ref, cache.lens, pos, 2 ** 32 + 8),
+                 lambda: cache.fork(pos.long()), lambda: cache.fork(pos[:2]), lambda: cache.reserve(pos.cpu()),
+                 lambda: paged.beam_select(logits, score, eos=2 ** 32), lambda: paged.beam_select(logits, score, eos=50),
+                 lambda: paged.beam_select(logits, score, n_out=10 ** 12),
+                 lambda: paged.beam_select(logits[:5], score)):
+        with pytest.raises(DexError) as e:
+            call()
+        assert e.value.status == DEX_E_INVAL
+    assert torch.equal(paged.rope(plan, pos, one), x)      # an input may be a broadcast one

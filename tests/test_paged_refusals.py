@@ -94,6 +94,24 @@ BAD = (
         (dict(requests=1 << 19), "2^20"), (dict(requests=1 << 17, beams=8, vocab=1 << 17, ld=1 << 17), "too many"),
         (dict(score=None), "NULL"), (dict(work=None), "NULL"), (dict(work=FAKE + 8), "aligned"),
         (dict(logits=FAKE + 1), "aligned")]]
+    # arrays off their type's alignment
+    + [(f, b, {n: b[n] + 2 if n != "plan" else dict(PLAN, turns=FAKE + 4)}, "aligned to") for f, b, names in [
+        ("dex_rope", ROPE, "pos plan"), ("dex_pages_append", APPEND, "pos table plan"),
+        ("dex_pages_attention", ATTENTION, "lens table"), ("dex_pages_fork", FORK, "table ref length parent t r n"),
+        ("dex_pages_reserve", RESERVE, "table ref length n_new pos src dst tokens state"),
+        ("dex_pages_compact", COMPACT, "table ref t r map src dst state"), ("dex_pages_copy", COPY, "src dst"),
+        ("dex_beam_select", BEAM, "score parent token score_out")] for n in names.split()]
+    + [(f, b, {n: b[n] + 1}, "aligned to its type") for f, b, names in [
+        ("dex_rope", ROPE, "q q_out k k_out"), ("dex_pages_append", APPEND, "q q_out k v"),
+        ("dex_pages_attention", ATTENTION, "q out")] for n in names.split()]
+    + [("dex_pages_attention", ATTENTION, dict(seq=FAKE + 1), "aligned"), ("dex_pages_append", APPEND, dict(seq=FAKE + 2), "aligned"),
+       ("dex_pages_attention", ATTENTION, dict(lse=FAKE + 2), "aligned"), ("dex_pages_copy", COPY, dict(tokens=FAKE + 2), "aligned"),
+       ("dex_pages_copy", COPY, dict(count=FAKE + 3), "aligned")]
+    # outputs whose rows or heads lie over each other (4 heads of 64, 2 rows)
+    + [(f, b, dict(zip(names.split(), st)), "overlap") for f, b, names in [
+        ("dex_rope", ROPE, "qo_row qo_head"), ("dex_rope", ROPE, "ko_row ko_head"), ("dex_pages_append", APPEND, "qo_row qo_head"),
+        ("dex_pages_attention", ATTENTION, "o_row o_head")]
+       for st in [(0, 64), (1 << 20, 0), (63, 128), (1 << 20, 63), (0, 0), (-1, 64), (64, 64), (2 ** 63 - 1, 63), (-2 ** 63, 1)]]
 )
 
 
@@ -120,6 +138,8 @@ def test_work_sizes(lib):
     assert lib.dex_pages_attention_work(1 << 20, 32, 8, 128, 1 << 20, 1) < 1 << 30   # rows go a few hundred at a time
     assert lib.dex_beam_select_work(1, 2, 4, 500, 4) > 0
     assert lib.dex_beam_select_work(7, 2, 4, 500, 4) == 0
+    assert lib.dex_beam_select_work(1, 1 << 30, 64, 500, 4) == 0        # sizes that the call refuses
+    assert lib.dex_beam_select_work(1, 2, 4, 500, 65) == 0
 
 
 def test_the_largest_max_len_needs_the_work_of_a_long_one(lib):
@@ -149,7 +169,7 @@ def test_turns_are_the_frequencies(lib, kw, rot):
 @pytest.mark.parametrize("args", [(4, 64, 1e4, 1, 1, 1, 2), (-1, 64, 1e4, 1, 1, 1, 2), (0, 63, 1e4, 1, 1, 1, 2),
                                   (0, 0, 1e4, 1, 1, 1, 2), (0, 64, 0.0, 1, 1, 1, 2), (0, 64, math.nan, 1, 1, 1, 2),
                                   (1, 64, 1e4, 0.0, 1, 1, 2), (1, 64, 1e4, math.inf, 1, 1, 2), (2, 2, 1e4, 4, 1, 1, 2),
-                                  (3, 64, 1e4, 4, 0.0, 1, 2), (3, 64, 1e4, 4, 4096, 2, 2), (3, 64, 1e4, 4, 4096, -1, 2)])
+                                  (0, 64, 1e-323, 1, 1, 1, 2), (1, 64, 1e4, 1e-323, 1, 1, 2), (3, 64, 1e4, 4, 0.0, 1, 2), (3, 64, 1e4, 4, 4096, 2, 2), (3, 64, 1e4, 4, 4096, -1, 2)])
 def test_bad_plans_are_refused(lib, args):
     assert lib.dex_rotary_turns(*args, (ctypes.c_double * 64)()) == dexlib.DEX_E_INVAL
     assert lib.dex_last_error(None).decode().startswith("dex_rotary_turns: ")
