@@ -60,10 +60,10 @@ __host__ __device__ __forceinline__ RowPlan row_plan(int len, int window) {
 constexpr int kSplitKeys = PA_UNIT * PA_WAVES;              // keys of a split, times 2^shift
 
 // A wave's: the values (or keys) of a unit, then its part of a split's sums.
-template <typename T, int HD>
+template <typename T, int HD, int NB>
 union Lds {
   uint16_t v[sizeof(T) == 2 ? PA_UNIT : 1][HD + 16];
-  float o[16][HD + 4];
+  float o[16 * NB][HD + 4];
 };
 // Barrier for what the workgroup's waves leave each other in LDS; loads from
 // memory stay on their way across it.
@@ -184,7 +184,7 @@ struct Wave<uint16_t, HD, NB, RUN> {
       }
     }
   }
-  __device__ __forceinline__ static void stage(const uint4 (&x)[V4], Lds<uint16_t, HD> &lds) {
+  __device__ __forceinline__ static void stage(const uint4 (&x)[V4], Lds<uint16_t, HD, NB> &lds) {
     const int lane = threadIdx.x & 63;
     uint16_t *to = &lds.v[lane / V4][(lane % V4) * 8];       // the rest are constants of the instructions
 #pragma unroll
@@ -196,8 +196,8 @@ struct Wave<uint16_t, HD, NB, RUN> {
     if constexpr (kTurns) load(base, rows, k);
     else load(base, rows, v);
   }
-  __device__ __forceinline__ void stage_k(Lds<uint16_t, HD> &lds) const { stage(k, lds); }
-  __device__ __forceinline__ void scores(int nb_used, pf_f32x4 (&sc)[NB][NT], const Lds<uint16_t, HD> &lds) const {
+  __device__ __forceinline__ void stage_k(Lds<uint16_t, HD, NB> &lds) const { stage(k, lds); }
+  __device__ __forceinline__ void scores(int nb_used, pf_f32x4 (&sc)[NB][NT], const Lds<uint16_t, HD, NB> &lds) const {
     const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
     const uint16_t *from = &lds.v[r16][grp * 8];
 #pragma unroll
@@ -216,12 +216,12 @@ struct Wave<uint16_t, HD, NB, RUN> {
     }
   }
   // values to LDS, those of absent keys as zeros (0 times NaN is not 0)
-  __device__ __forceinline__ void stage_v(unsigned long long mask, bool full, Lds<uint16_t, HD> &lds) {
+  __device__ __forceinline__ void stage_v(unsigned long long mask, bool full, Lds<uint16_t, HD, NB> &lds) {
     if constexpr (kTurns) stage_masked(k, mask, full, lds);
     else stage_masked(v, mask, full, lds);
   }
   __device__ __forceinline__ static void stage_masked(uint4 (&x)[V4], unsigned long long mask, bool full,
-                                                      Lds<uint16_t, HD> &lds) {
+                                                      Lds<uint16_t, HD, NB> &lds) {
     if (!full) {
       const unsigned long long mine = mask >> ((threadIdx.x & 63) / V4);
 #pragma unroll
@@ -230,7 +230,7 @@ struct Wave<uint16_t, HD, NB, RUN> {
     }
     stage(x, lds);
   }
-  __device__ __forceinline__ void outputs(int nb, const pf_f32x4 (&p)[NT], const Lds<uint16_t, HD> &lds) {
+  __device__ __forceinline__ void outputs(int nb, const pf_f32x4 (&p)[NT], const Lds<uint16_t, HD, NB> &lds) {
     const int lane = threadIdx.x & 63, tq = lane >> 4, ti = (lane & 15) >> 2, tg = lane & 3;
     const uint16_t *from = &lds.v[4 * tq + ti][4 * tg];
 #pragma unroll
@@ -312,8 +312,8 @@ struct Wave<float, HD, NB, RUN> {
         for (int b = 0; b < VB; ++b) v[nt][i][b] = *(const vecw *)(p + off + b * (64 * W));
       }
   }
-  __device__ __forceinline__ void stage_k(Lds<float, HD> &) const {}
-  __device__ __forceinline__ void scores(int nb_used, pf_f32x4 (&sc)[NB][NT], const Lds<float, HD> &) const {
+  __device__ __forceinline__ void stage_k(Lds<float, HD, NB> &) const {}
+  __device__ __forceinline__ void scores(int nb_used, pf_f32x4 (&sc)[NB][NT], const Lds<float, HD, NB> &) const {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
       if (nb < nb_used) {
@@ -328,7 +328,7 @@ struct Wave<float, HD, NB, RUN> {
         }
       }
   }
-  __device__ __forceinline__ void stage_v(unsigned long long mask, bool full, Lds<float, HD> &) {
+  __device__ __forceinline__ void stage_v(unsigned long long mask, bool full, Lds<float, HD, NB> &) {
     if (!full) {
       const unsigned long long mine = mask >> (4 * ((threadIdx.x & 63) >> 4));
 #pragma unroll
@@ -340,7 +340,7 @@ struct Wave<float, HD, NB, RUN> {
             if (!(mine >> (nt * 16 + i) & 1)) v[nt][i][b] = (vecw)0.f;
     }
   }
-  __device__ __forceinline__ void outputs(int nb, const pf_f32x4 (&p)[NT], const Lds<float, HD> &) {
+  __device__ __forceinline__ void outputs(int nb, const pf_f32x4 (&p)[NT], const Lds<float, HD, NB> &) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -405,7 +405,7 @@ __device__ __forceinline__ int group_rows(const Sharing &g, int r, int n_rows) {
 
 // The leading splits that are the same keys for every row of a group: one
 // workgroup compares their table rows (6 us; 16 x 8 rows that share 4000 of 4090
-// keys then take 85 + 9 us, alone 261 + 32).  They are the same work only where all
+// keys then take 84 + 8.5 us, alone 261 + 32).  They are the same work only where all
 // rows are cut alike and see all of the split, or all have one length.
 __global__ __launch_bounds__(PA_THREADS) void paged_share_kernel(PagedAttnArgs a, Sharing g, int *share) {
   __shared__ int lens[PA_COLS], seqs[PA_COLS], first;
@@ -465,16 +465,16 @@ __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2
                                                                  float2 *stat) {
   using W = Wave<T, HD, NB, RUN>;
   constexpr int UNIT_TILES = PA_UNIT / W::TK;
-  // (the LDS below is at most half of a compute unit's 160 KiB, 80.4 KB at
+  // (the LDS below is at most half of a compute unit's 160 KiB, 80.9 KB at
   // head_dim 128 in bf16; with 82.5 KB one workgroup a unit was left and 8 x
   // 8300 keys took 77 us for 62)
-  __shared__ Lds<T, HD> lds_all[PA_WAVES];
+  __shared__ Lds<T, HD, NB> lds_all[PA_WAVES];
   __shared__ int first_item[PA_ROWS], keys_of[PA_ROWS], share_of[PA_ROWS];   // items before a row's; its keys
   __shared__ int part[PA_WAVES];
-  __shared__ float wm[PA_WAVES][16], wl[PA_WAVES][16];
+  __shared__ float wm[PA_WAVES][16 * NB], wl[PA_WAVES][16 * NB];
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  Lds<T, HD> &lds = lds_all[wave];
+  Lds<T, HD, NB> &lds = lds_all[wave];
   const int kv = a.map.n_kv_heads, G = a.n_heads / kv;
   const int chunks = (G + PA_COLS - 1) / PA_COLS, per_split = kv * chunks;   // items of a split
   const float scale2 = a.scale * kLog2e;
@@ -633,56 +633,55 @@ __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2
     if constexpr (sizeof(T) == 4) w.load_v(a.v, there(rows1));
     else wave_lds_sync();                 // the values are read before anything takes their place
     if (last) {
-      // the four waves' sums under one reference, 16 columns at a time
+      // the four waves' sums under one reference
+      const int cols = cur.rows * cur.cols;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const int used = min(16, cur.rows * cur.cols - nb * 16);
-        if (used <= 0) break;
+        const int c = nb * 16 + r16;
         const float sum = quad_sum(l[nb]);
-        if (r16 < used) {
+        if (c < cols) {
           if (grp == 0) {
-            wm[wave][r16] = m[nb];
-            wl[wave][r16] = sum;
+            wm[wave][c] = m[nb];
+            wl[wave][c] = sum;
           }
 #pragma unroll
           for (int dt = 0; dt < W::DT; ++dt) {
             if constexpr (W::kRun == 4) {
-              *(pf_f32x4 *)&lds.o[r16][W::dim(dt, 0)] = w.o[nb][dt];
+              *(pf_f32x4 *)&lds.o[c][W::dim(dt, 0)] = w.o[nb][dt];
             } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) lds.o[r16][W::dim(dt, i)] = w.o[nb][dt][i];
+              for (int i = 0; i < 4; ++i) lds.o[c][W::dim(dt, i)] = w.o[nb][dt][i];
             }
           }
         }
-        lds_barrier();
-        for (int e = tid; e < used * (HD / 4); e += PA_THREADS) {
-          const int c = e / (HD / 4), d = e % (HD / 4) * 4;
-          float mm = wm[0][c];
-#pragma unroll
-          for (int v = 1; v < PA_WAVES; ++v) mm = fmaxf(mm, wm[v][c]);
-          const float ref = mm == -INFINITY ? 0.f : mm;
-          pf_f32x4 o = {0.f, 0.f, 0.f, 0.f};
-          float ll = 0.f;
-#pragma unroll
-          for (int v = 0; v < PA_WAVES; ++v) {
-            const float f = __builtin_amdgcn_exp2f(wm[v][c] - ref);
-            const pf_f32x4 x = *(const pf_f32x4 *)&lds_all[v].o[c][d];
-            ll = fmaf(f, wl[v][c], ll);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = fmaf(f, x[i], o[i]);
-          }
-          const int col = nb * 16 + c, i = col / cur.cols;
-          const int row = cur.row + i, head = cur.head0 + col - i * cur.cols;
-          if (cur.n == 1) {
-            finish<T, RUN>(a, row, head, d, o, mm, ll);
-          } else {
-            const size_t at = rec_index(a, row, head, cur.split, smax);
-            *(pf_f32x4 *)(rec + at * HD + d) = o;
-            if (d == 0) stat[at] = make_float2(mm, ll);
-          }
-        }
-        lds_barrier();
       }
+      lds_barrier();
+      for (int e = tid; e < cols * (HD / 4); e += PA_THREADS) {
+        const int c = e / (HD / 4), d = e % (HD / 4) * 4;
+        float mm = wm[0][c];
+#pragma unroll
+        for (int v = 1; v < PA_WAVES; ++v) mm = fmaxf(mm, wm[v][c]);
+        const float ref = mm == -INFINITY ? 0.f : mm;
+        pf_f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        float ll = 0.f;
+#pragma unroll
+        for (int v = 0; v < PA_WAVES; ++v) {
+          const float f = __builtin_amdgcn_exp2f(wm[v][c] - ref);
+          const pf_f32x4 x = *(const pf_f32x4 *)&lds_all[v].o[c][d];
+          ll = fmaf(f, wl[v][c], ll);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = fmaf(f, x[i], o[i]);
+        }
+        const int i = c / cur.cols, row = cur.row + i, head = cur.head0 + c - i * cur.cols;
+        if (cur.n == 1) {
+          finish<T, RUN>(a, row, head, d, o, mm, ll);
+        } else {
+          const size_t at = rec_index(a, row, head, cur.split, smax);
+          *(pf_f32x4 *)(rec + at * HD + d) = o;
+          if (d == 0) stat[at] = make_float2(mm, ll);
+        }
+      }
+      lds_barrier();
       if (nxt.item >= items) break;
       clear();
     }
