@@ -21,6 +21,7 @@ constexpr int WAVES = 4;                  // of a segment workgroup
 constexpr int LIST = 252;                 // candidates a wave sorts
 constexpr int LIST_ROOM = LIST + 4;
 constexpr int JOIN_WAVES = 8;
+constexpr int HOLD = 32;                  // lanes whose logits go through LDS
 
 struct Cand {
   uint32_t key;                           // order-preserving bits of the logit; 0: none
@@ -87,6 +88,19 @@ __device__ __forceinline__ uint32_t nth_of_lanes(uint32_t key, int n) {
 template <typename F>
 __device__ __forceinline__ void rank_list(Cand *list, int cnt, F f) {
   const int lane = threadIdx.x & 63;
+  if (cnt <= 64) {                        // one a lane: no more round trips to LDS
+    wave_sync();
+    const Cand c = lane < cnt ? list[lane] : Cand{0u, -1};
+    const uint64_t mine = (uint64_t)c.key << 32 | ~(uint32_t)c.idx;
+    int r = 0;
+    for (int j = 0; j < cnt; ++j) {
+      const uint64_t o = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)c.key, j) << 32 |
+                         ~(uint32_t)__builtin_amdgcn_readlane(c.idx, j);
+      r += o > mine ? 1 : 0;
+    }
+    if (lane < cnt) f(r, c);
+    return;
+  }
   if (lane < 3) list[cnt + lane] = Cand{0u, -1};  // ranks before nothing
   wave_sync();
   for (int i = lane; i < cnt; i += 64) {
@@ -116,12 +130,13 @@ __host__ __device__ inline int segments(int vocab, int grain, int seg) { return 
 // A wave takes a segment of 64 LANE logits, LANE a lane, all in registers.
 // What bounds it is the instructions: a logit takes a conversion, the maximum,
 // the exponential's four and one comparison with the threshold below, a wave
-// about 300 more.  320 rows of 65537 bf16 logits (42 MB, 8 us at a copy's rate)
-// take 19 us; 4 rows of 32000 floats 4.3 us, the latency of one wave.
+// about 200 more.  320 rows of 65537 bf16 logits (42 MB, 8 us at a copy's rate)
+// take 18 us; 4 rows of 32000 floats 3.9 us, the latency of one wave.
 template <typename T, int LANE>
 __global__ __launch_bounds__(WAVES * 64, 5) void beam_segment_kernel(BeamArgs a, int n_seg, Cand *cand, SegStat *stat) {
   constexpr int GR = kGrain<T>, IT = LANE / GR, SEG = 64 * LANE;
   __shared__ Cand lists[WAVES][LIST_ROOM];
+  __shared__ __align__(16) float holds[WAVES][HOLD][LANE + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int blocks = (n_seg + WAVES - 1) / WAVES;          // of a row
   const int row = blockIdx.x / blocks;
@@ -208,14 +223,39 @@ __global__ __launch_bounds__(WAVES * 64, 5) void beam_segment_kernel(BeamArgs a,
   };
   // absent places hold -inf: only what is above that goes by its value alone
   const float tf = of_key(max(t, none + 1));
+  const unsigned long long have = __ballot(top >= tf);
+  const int n_have = __popcll(have);
+  if (n_have <= HOLD) {
+    // few lanes reach t: theirs go through LDS and are spread over the wave (a
+    // ballot for each of the LANE places takes 3 to 5 % longer)
+    float(*hold)[LANE + 4] = holds[wave];
+    if (top >= tf) {
+      float *to = hold[__popcll(have & lt)];
 #pragma unroll
-  for (int k = 0; k < LANE; ++k) {
-    const bool in = v[k] >= tf;
-    const unsigned long long b = __ballot(in);
-    if (b != 0) {
+      for (int k = 0; k < LANE; k += 4) *(float4 *)(to + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+      to[LANE] = __int_as_float(token(0));
+    }
+    wave_sync();
+    for (int f0 = 0; f0 < n_have * LANE; f0 += 64) {
+      const int f = f0 + lane, r = f / LANE, k = f % LANE;
+      const float x1 = f < n_have * LANE ? hold[r][k] : -INFINITY;
+      const bool in = x1 >= tf;
+      const unsigned long long b = __ballot(in);
+      if (b == 0) continue;
       const int p = cnt + __popcll(b & lt);
-      if (in && p < LIST) list[p] = Cand{key_of(v[k]), token(k)};
+      if (in && p < LIST) list[p] = Cand{key_of(x1), __float_as_int(hold[r][LANE]) + k / GR * 64 * GR + k % GR};
       cnt += __popcll(b);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < LANE; ++k) {
+      const bool in = v[k] >= tf;
+      const unsigned long long b = __ballot(in);
+      if (b != 0) {
+        const int p = cnt + __popcll(b & lt);
+        if (in && p < LIST) list[p] = Cand{key_of(v[k]), token(k)};
+        cnt += __popcll(b);
+      }
     }
   }
   if (cnt > LIST) {
