@@ -138,10 +138,8 @@ __global__ __launch_bounds__(WAVES * 64, 5) void beam_segment_kernel(BeamArgs a,
   __shared__ Cand lists[WAVES][LIST_ROOM];
   __shared__ __align__(16) float holds[WAVES][HOLD][LANE + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int blocks = (n_seg + WAVES - 1) / WAVES;          // of a row
-  const int row = blockIdx.x / blocks;
-  const int seg = (blockIdx.x - row * blocks) * WAVES + wave;
-  if (seg >= n_seg) return;
+  const int item = blockIdx.x * WAVES + wave, row = item / n_seg, seg = item - row * n_seg;
+  if (row >= a.requests * a.beams) return;
   if (a.done != nullptr && a.done[row]) return;   // the second kernel asks nothing of it
   const T *x = (const T *)a.logits + (int64_t)row * a.ld;
   // place 0 of the grains is the 16-byte boundary at or before the row: the
@@ -442,7 +440,7 @@ hipError_t launch_beam(int dtype, const BeamArgs &a, hipStream_t s) {
   const int n_seg = segments(a.vocab, dtype == DEX_F32 ? kGrain<float> : kGrain<uint16_t>, 64 * lane);
   Cand *cand = (Cand *)a.work;
   SegStat *stat = (SegStat *)(cand + (size_t)rows * n_seg * a.n_out);
-  const unsigned grid = (unsigned)((n_seg + WAVES - 1) / WAVES) * rows;
+  const unsigned grid = (unsigned)((rows * n_seg + WAVES - 1) / WAVES);
   if (dtype == DEX_F32) {
     if (lane == 8) beam_segment_kernel<float, 8><<<grid, WAVES * 64, 0, s>>>(a, n_seg, cand, stat);
     else beam_segment_kernel<float, 32><<<grid, WAVES * 64, 0, s>>>(a, n_seg, cand, stat);
