@@ -28,6 +28,7 @@ A step of a decoding loop with branches, for a model of the caller's:
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 from typing import NamedTuple
 
@@ -47,6 +48,17 @@ def _refuse(why: str):
 # The current stream's handle: torch's own short cut to it where it has one
 # (0.1 us a call; building a Stream object takes 2 to 3 of a small call's 12).
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+# Work memory by a call's sizes, asked once for each (0.6 us of a small call's 17).
+@functools.lru_cache(maxsize=4096)
+def _attention_work(*sizes):
+    return dexlib.load().dex_pages_attention_work(*sizes)
+
+
+@functools.lru_cache(maxsize=4096)
+def _beam_work(*sizes):
+    return max(16, dexlib.load().dex_beam_select_work(*sizes))
 
 
 def _run(fn, device, *args):
@@ -225,10 +237,9 @@ def attention(q, k_pages, v_pages, table, lens, seq=None, max_len=None, scale=No
         _refuse("max_len or window is below 0, or group below 1, or past 2^31 - 1")
     lse = torch.empty((rows, heads), dtype=torch.float32, device=dev) if return_lse else None
     if rows > 0:
-        lib = dexlib.load()
-        size = lib.dex_pages_attention_work(rows, heads, kv, hd, max_len, group)
+        size = _attention_work(rows, heads, kv, hd, max_len, group)
         work = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
-        _run(lib.dex_pages_attention, dev, d, hd, heads, kv, rows, s, n, max_len, window, group,
+        _run(dexlib.load().dex_pages_attention, dev, d, hd, heads, kv, rows, s, n, max_len, window, group,
              1.0 / math.sqrt(hd) if scale is None else scale, *a, k_pages.data_ptr(), v_pages.data_ptr(), n_pages, ps, tab,
              ts[0], ts[1], *o, None if lse is None else lse.data_ptr(), None if work is None else work.data_ptr())
     return (out, lse) if return_lse else out
@@ -364,9 +375,8 @@ def beam_select(logits, scores, n_out=None, done=None, eos=-1):
     parent = torch.empty_like(score, dtype=torch.int32)
     token, ends = torch.empty_like(parent), torch.empty_like(score, dtype=torch.bool)
     if requests > 0:
-        lib = dexlib.load()
-        work = torch.empty(max(16, lib.dex_beam_select_work(d, requests, beams, vocab, n)), dtype=torch.uint8, device=dev)
-        _run(lib.dex_beam_select, dev, d, logits.data_ptr(), ld, requests, beams, vocab, scores.data_ptr(),
+        work = torch.empty(_beam_work(d, requests, beams, vocab, n), dtype=torch.uint8, device=dev)
+        _run(dexlib.load().dex_beam_select, dev, d, logits.data_ptr(), ld, requests, beams, vocab, scores.data_ptr(),
              None if done is None else done.data_ptr(), eos, n, parent.data_ptr(), token.data_ptr(), score.data_ptr(),
              ends.data_ptr(), work.data_ptr())
     return parent, token, score, ends
