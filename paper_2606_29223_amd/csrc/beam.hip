@@ -422,9 +422,9 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void beam_join_kernel(BeamArgs a, 
 
 // Logits of a lane: 32, or 8 where that leaves the join of a row one segment a
 // lane and the GPU's 1024 SIMDs at most a wave each, so that a call is one wave's
-// time. 8 against 32, bf16, us: 4 rows of 8000 logits 9.2 / 10.5, of 32000 9.5 /
-// 10.2, 16 rows of 32000 13.1 / 13.5; past either limit 8 rows of 65000 16.7 /
-// 13.6, 64 rows of 32000 14.4 / 13.9, 512 rows 30.3 / 23.0.
+// time. 8 against 32, bf16, us: 4 rows of 8000 logits 8.7 / 10.1, of 32000 9.0 /
+// 9.6, 16 rows of 32000 12.7 / 13.1; past either limit 8 rows of 65000 16.5 /
+// 13.2, 64 rows of 32000 13.9 / 13.4, 512 rows 28.1 / 22.5.
 static int lane_logits(int rows, int vocab) {
   const int n_seg = segments(vocab, 8, 64 * 8);
   return n_seg <= 64 && (int64_t)rows * n_seg <= 1024 ? 8 : 32;
