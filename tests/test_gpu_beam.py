@@ -75,6 +75,32 @@ def test_masked_vocabularies(dtype):
         _run(x, -rng.random((2, 3)), 12)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [9000, 40001])          # 8 logits a lane, and 32
+def test_candidates_in_few_lanes_and_in_all(dtype, vocab):
+    """The best logits in some lanes of a wave only (tokens by their 16-byte
+    grain), fewer and more of them than a list holds; few values; masks."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(vocab)
+    grain = 8 if dtype == "bf16" else 4
+    lane = np.arange(vocab) // grain % 64
+    base = rng.random((6, vocab))
+    for lanes in (1, 3, 32, 33):
+        x = np.where(lane < lanes, 10 + base, base)
+        x[:, lane == 0] = np.minimum(x[:, lane == 0], 10.25)     # most of the other lanes' are above its maximum
+        for n_out in (1, lanes, 64):
+            _run(torch.from_numpy(x.astype(np.float32)).to(dtype_of(dtype)).cuda(), -rng.random((2, 3)), n_out)
+    few = torch.from_numpy(rng.integers(0, 3, (6, vocab)).astype(np.float32)).to(dtype_of(dtype)).cuda()
+    for n_out in (3, 40, 64):
+        _run(few, np.zeros((2, 3)), n_out)
+    for keep in ([], [vocab - 1], list(range(vocab - 70, vocab)), list(range(1, vocab, 2))):
+        x = torch.full((6, vocab), -math.inf, dtype=dtype_of(dtype), device="cuda")
+        if keep:
+            x[:, keep] = _logits(rng, 6, len(keep), dtype)
+        for n_out in (3, 40):
+            _run(x, -rng.random((2, 3)), n_out)
+
+
 def test_finished_first_and_hopeless_beams():
     torch = torch_cuda()
     rng = np.random.default_rng(9)
