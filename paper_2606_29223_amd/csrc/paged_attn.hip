@@ -41,6 +41,7 @@ constexpr int PA_UNIT = 64;               // keys of a unit
 constexpr int PA_SPLITS = 24;             // splits of a row at most
 constexpr int PA_ROWS = 512;              // rows of a launch
 constexpr int PA_COLS = 32;               // query heads of an item
+constexpr int kAlone = 256;               // in share_of: the row is one split (of PA_SPLITS at most)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // How a row of `len` keys is cut: units [unit0, unit0 + units), 2^shift a run.
@@ -457,7 +458,6 @@ struct Place {
   int item;                               // >= the number of items: nowhere
   int row, rows, head, head0, cols, split, seq, lo, len;   // kv head; first query head; heads a row
   int tile, tiles, key, end;              // of the run; this wave's first key of the tile; the row's end
-  int n;                                  // splits of the row
 };
 
 template <typename T, int HD, int NB, int RUN>
@@ -489,8 +489,8 @@ __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2
       const int len = r < a.n_rows ? row_keys(a, r) : 0;
       const int sh = g.share != nullptr && r < a.n_rows ? g.share[r] : 0;
       keys_of[r] = len;
-      share_of[r] = sh;
       int c = row_plan(len, a.window).n;
+      share_of[r] = c == 1 ? sh | kAlone : sh;
       if (sh > 0 && place_in_group(g, r) > 0) c -= sh;
       n[k] = r < a.n_rows ? c * per_split : 0;
       sum += n[k];
@@ -534,7 +534,7 @@ __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2
     p.head0 = p.head * G + chunk * PA_COLS;
     p.cols = min(PA_COLS, G - chunk * PA_COLS);
     p.rows = 1;
-    const int sh = __builtin_amdgcn_readfirstlane(share_of[lo]);
+    const int sh = __builtin_amdgcn_readfirstlane(share_of[lo]) & (kAlone - 1);
     if (sh > 0) {
       if (place_in_group(g, lo) > 0) p.split += sh;
       else if (p.split < sh) p.rows = group_rows(g, lo, a.n_rows);
@@ -542,7 +542,6 @@ __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2
     p.seq = a.seq != nullptr ? __builtin_amdgcn_readfirstlane(a.seq[lo]) : lo;
     const RowPlan pl = row_plan(p.len, a.window);
     p.lo = pl.lo;
-    p.n = pl.n;
     p.tile = 0;
     p.tiles = UNIT_TILES << pl.shift;
     p.key = (pl.unit0 + ((p.split * PA_WAVES + wave) << pl.shift)) * PA_UNIT;
@@ -655,6 +654,12 @@ __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2
           }
         }
       }
+      // The item's rows that are this split alone: output or record goes by the
+      // row's own number of splits, as its join does, for of rows that share a
+      // split one may end with it (256 keys) where others go on.  (Worked out
+      // from each row's length below it spills six registers, 69 us for 62 at 8
+      // x 8300 keys.)
+      const unsigned long long alone = __ballot(lane < cur.rows && share_of[cur.row + lane] >= kAlone);
       lds_barrier();
       for (int e = tid; e < cols * (HD / 4); e += PA_THREADS) {
         const int c = e / (HD / 4), d = e % (HD / 4) * 4;
@@ -673,7 +678,7 @@ __global__ __launch_bounds__(PA_THREADS, sizeof(T) == 4 && HD * NB > 128 ? 1 : 2
           for (int i = 0; i < 4; ++i) o[i] = fmaf(f, x[i], o[i]);
         }
         const int i = c / cur.cols, row = cur.row + i, head = cur.head0 + c - i * cur.cols;
-        if (cur.n == 1) {
+        if (alone >> i & 1) {
           finish<T, RUN>(a, row, head, d, o, mm, ll);
         } else {
           const size_t at = rec_index(a, row, head, cur.split, smax);
