@@ -15,9 +15,10 @@
 // A unit is S^T = K Q^T and O^T = V^T P^T on the matrix cores, the kv head's
 // query heads as columns, so that each lane holds the scores and outputs of
 // one query head.  Keys and values are read once from HBM, which bounds the
-// kernel; the products are 4 % of what the matrix cores could do meanwhile.
-// That is why P goes through them in two bf16 parts (p = hi + lo to 2^-17): it
-// costs the output no accuracy and no time.
+// kernel; the products are 5 % of what the matrix cores could do meanwhile.
+// That is why P goes through them in three bf16 parts, which are all of its 24
+// bits, so that weights are as exact as in fp32: against two parts (2^-17) it
+// costs 0 to 3 % (16 x 2000 keys 37.5 and 38.2 us, 8 x 8300 62.6 and 62.5).
 //
 // Measured (32 / 8 heads of 128, bf16): 8 rows of 8300 keys 56.8 us and the join
 // 4.7 for 272 MB, 4.8 TB/s in the kernel; 64 rows of 1 to 16000 keys 99 + 4.9
@@ -139,6 +140,13 @@ __device__ __forceinline__ const char *row_at(const void *base, uint32_t rows, i
   return (const char *)base + (uint64_t)(uint32_t)__shfl((int)rows, j, 64) * (HD * sizeof(T));
 }
 
+// A float's upper half is a bf16, and what is left of its 24 bits after that two
+// more: three parts that are the float, with no rounding.
+__device__ __forceinline__ uint32_t upper_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ float after_upper(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xffff0000u); }
+
 // bf16: a tile is a unit.  Keys and values come as whole rows, 1 KB a load
 // (keys in fragment order are sixteen 64-byte pieces, 4 % slower), and go
 // through LDS: keys are read back as fragments, values transposed.
@@ -150,6 +158,11 @@ struct Wave<uint16_t, HD, NB, RUN> {
   // values on their way, not both: then both use k, in turns.
   static constexpr bool kTurns = HD * NB > 128;
   uint4 k[V4], v[kTurns ? 1 : V4];
+  // Values of a product read from LDS ahead of their use: the next tile is in
+  // registers, and with more the compiler spills (two column blocks with four:
+  // 105 us for 99 at 16 x 8 beams; an address a lane with four: 52 for 44 at 16 x
+  // 2000 keys).
+  static constexpr int kReads = NB > 1 ? 2 : RUN > 1 ? 4 : 1;
   pf_f32x4 o[NB][DT];
 
   // a column's query, from `src` (null: none)
@@ -236,22 +249,28 @@ struct Wave<uint16_t, HD, NB, RUN> {
     const uint16_t *from = &lds.v[4 * tq + ti][4 * tg];
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-      uint32_t hi[4], lo[4];
+      if constexpr (NB > 1) __builtin_amdgcn_sched_barrier(0);
+      uint32_t part[3][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float a = p[2 * st + i / 2][2 * (i % 2)], b = p[2 * st + i / 2][2 * (i % 2) + 1];
-        hi[i] = pf_pack_bf16(a, b);
-        lo[i] = pf_pack_bf16(a - __uint_as_float(hi[i] << 16), b - __uint_as_float(hi[i] & 0xffff0000u));
+        float a = p[2 * st + i / 2][2 * (i % 2)], b = p[2 * st + i / 2][2 * (i % 2) + 1];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          part[k][i] = upper_halves(a, b);
+          a = after_upper(a);
+          b = after_upper(b);
+        }
       }
-      const pf_bf16x8 ph = __builtin_bit_cast(pf_bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-      const pf_bf16x8 pl = __builtin_bit_cast(pf_bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+      pf_bf16x8 pp[3];
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        pp[k] = __builtin_bit_cast(pf_bf16x8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3]));
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const pf_bf16x8 vf = tr_frag(from + 32 * st * (HD + 16) + 16 * dt, from + (32 * st + 16) * (HD + 16) + 16 * dt);
-        o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph, o[nb][dt], 0, 0, 0);
-        o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl, o[nb][dt], 0, 0, 0);
-        // not all of the tile's reads at once: the next tile is in registers
-        if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[k], o[nb][dt], 0, 0, 0);
+        if (dt % kReads == kReads - 1) __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
