@@ -141,11 +141,15 @@ __device__ __forceinline__ const char *row_at(const void *base, uint32_t rows, i
 }
 
 // A float's upper half is a bf16, and what is left of its 24 bits after that two
-// more: three parts that are the float, with no rounding.
+// more: three parts that are the float, with no rounding.  Where nothing is left
+// a part is 2^-100, not 0, so that an infinite value times its weight, the sum
+// over the parts, is infinite (0 and negative parts would make it NaN).
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
-__device__ __forceinline__ float after_upper(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xffff0000u); }
+__device__ __forceinline__ float after_upper(float a) {
+  return fmaxf(a - __uint_as_float(__float_as_uint(a) & 0xffff0000u), 0x1p-100f);
+}
 
 // bf16: a tile is a unit.  Keys and values come as whole rows, 1 KB a load
 // (keys in fragment order are sixteen 64-byte pieces, 4 % slower), and go
