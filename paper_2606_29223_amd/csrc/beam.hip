@@ -124,8 +124,17 @@ struct SegStat {
 template <typename T>
 constexpr int kGrain = 16 / (int)sizeof(T);       // logits of a 16-byte load
 
-// Segments of a row: its logits may begin anywhere in their first 16 bytes.
-__host__ __device__ inline int segments(int vocab, int grain, int seg) { return (vocab + grain - 1 + seg - 1) / seg; }
+inline int segments(int vocab, int seg) { return (vocab + seg - 1) / seg; }
+
+// 16 bytes from any element on: segments are cut at tokens, not at boundaries of
+// memory, so that rows of the same logits have the same sums to the last bit,
+// wherever they begin (an odd vocabulary has them begin everywhere), and tie.
+template <typename T>
+__device__ __forceinline__ uint4 load_grain(const T *p) {
+  uint4 g;
+  __builtin_memcpy(&g, p, sizeof g);
+  return g;
+}
 
 // A wave takes a segment of 64 LANE logits, LANE a lane, all in registers.
 // What bounds it is the instructions: a logit takes a conversion, the maximum,
@@ -142,17 +151,15 @@ __global__ __launch_bounds__(WAVES * 64, 5) void beam_segment_kernel(BeamArgs a,
   if (row >= a.requests * a.beams) return;
   if (a.done != nullptr && a.done[row]) return;   // the second kernel asks nothing of it
   const T *x = (const T *)a.logits + (int64_t)row * a.ld;
-  // place 0 of the grains is the 16-byte boundary at or before the row: the
-  // token of a lane's k-th logit is at + k / GR * 64 * GR + k % GR
-  const int at = seg * SEG + lane * GR - (int)(((uintptr_t)x & 15) / sizeof(T));
-  const bool whole = seg * SEG >= GR && (seg + 1) * SEG <= a.vocab;       // every place is a token
+  const int at = seg * SEG + lane * GR;           // a lane's k-th logit is token at + k / GR * 64 * GR + k % GR
+  const bool whole = (seg + 1) * SEG <= a.vocab;  // every place is a token
   auto token = [&](int k) { return at + k / GR * 64 * GR + k % GR; };
-  auto exists = [&](int k) { return (unsigned)token(k) < (unsigned)a.vocab; };
+  auto exists = [&](int k) { return token(k) < a.vocab; };
   float v[LANE];
   if (whole) {
     uint4 raw[IT];
 #pragma unroll
-    for (int i = 0; i < IT; ++i) raw[i] = *(const uint4 *)(x + token(i * GR));
+    for (int i = 0; i < IT; ++i) raw[i] = load_grain(x + token(i * GR));
 #pragma unroll
     for (int k = 0; k < LANE; ++k) {
       const uint4 g = raw[k / GR];
@@ -161,10 +168,10 @@ __global__ __launch_bounds__(WAVES * 64, 5) void beam_segment_kernel(BeamArgs a,
       if constexpr (sizeof(T) == 2) v[k] = __uint_as_float(k & 1 ? w & 0xffff0000u : w << 16);
       else v[k] = __uint_as_float(w);
     }
-  } else {                                        // a row's ends: by elements, the same places
+  } else {                                        // a row's end: by elements, the same places
     T e[LANE];
 #pragma unroll
-    for (int k = 0; k < LANE; ++k) e[k] = x[min(max(token(k), 0), a.vocab - 1)];
+    for (int k = 0; k < LANE; ++k) e[k] = x[min(token(k), a.vocab - 1)];
 #pragma unroll
     for (int k = 0; k < LANE; ++k) {
       float f;
@@ -426,18 +433,18 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void beam_join_kernel(BeamArgs a, 
 // 9.6, 16 rows of 32000 12.7 / 13.1; past either limit 8 rows of 65000 16.5 /
 // 13.2, 64 rows of 32000 13.9 / 13.4, 512 rows 28.1 / 22.5.
 static int lane_logits(int rows, int vocab) {
-  const int n_seg = segments(vocab, 8, 64 * 8);
+  const int n_seg = segments(vocab, 64 * 8);
   return n_seg <= 64 && (int64_t)rows * n_seg <= 1024 ? 8 : 32;
 }
 
-size_t beam_work(int dtype, int rows, int vocab, int n_out) {
-  const size_t n_seg = segments(vocab, dtype == DEX_F32 ? kGrain<float> : kGrain<uint16_t>, 64 * lane_logits(rows, vocab));
+size_t beam_work(int rows, int vocab, int n_out) {
+  const size_t n_seg = segments(vocab, 64 * lane_logits(rows, vocab));
   return (size_t)rows * n_seg * (n_out * sizeof(Cand) + sizeof(SegStat));
 }
 
 hipError_t launch_beam(int dtype, const BeamArgs &a, hipStream_t s) {
   const int rows = a.requests * a.beams, lane = lane_logits(rows, a.vocab);
-  const int n_seg = segments(a.vocab, dtype == DEX_F32 ? kGrain<float> : kGrain<uint16_t>, 64 * lane);
+  const int n_seg = segments(a.vocab, 64 * lane);
   Cand *cand = (Cand *)a.work;
   SegStat *stat = (SegStat *)(cand + (size_t)rows * n_seg * a.n_out);
   const unsigned grid = (unsigned)((rows * n_seg + WAVES - 1) / WAVES);

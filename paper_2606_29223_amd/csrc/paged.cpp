@@ -300,7 +300,7 @@ dex_status dex_pages_copy(int32_t dtype, int32_t head_dim, int32_t n_layers, int
 int64_t dex_beam_select_work(int32_t dtype, int32_t requests, int32_t beams, int32_t vocab, int32_t n_out) {
   if (!known(dtype) || requests < 0 || beams < 1 || vocab < 1 || n_out < 1 || n_out > kMaxBeams) return 0;
   if ((int64_t)requests * beams > (1 << 20)) return 0;
-  return (int64_t)beam_work(dtype, (int64_t)requests * beams, vocab, n_out);
+  return (int64_t)beam_work(requests * beams, vocab, n_out);
 }
 
 dex_status dex_beam_select(int32_t dtype, const void *logits, int64_t ld, int32_t requests, int32_t beams, int32_t vocab,

@@ -124,7 +124,7 @@ struct BeamArgs {
   uint8_t *done_out;          // or null
   void *work;
 };
-size_t beam_work(int dtype, int rows, int vocab, int n_out);
+size_t beam_work(int rows, int vocab, int n_out);
 hipError_t launch_beam(int dtype, const BeamArgs &a, hipStream_t s);
 
 }  // namespace dex
