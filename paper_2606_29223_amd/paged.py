@@ -367,9 +367,8 @@ def copy(k_pool, v_pool, src, dst, count=None, tokens=None):
         if count.dim() != 1 or count.shape[0] < 1:
             _refuse("count holds the number of entries in its first element")
         num = _ints(count, dev, count.shape, "count")
-    if n > 0:
-        _run(dexlib.load().dex_pages_copy, dev, d, hd, layers, n_pages, kv, ps, k_pool.data_ptr(), v_pool.data_ptr(), s, t,
-             tok, num, n)
+    _run(dexlib.load().dex_pages_copy, dev, d, hd, layers, n_pages, kv, ps, k_pool.data_ptr(), v_pool.data_ptr(), s, t,
+         tok, num, n)
 
 
 def beam_select(logits, scores, n_out=None, done=None, eos=-1):
@@ -417,9 +416,19 @@ class PagedCache:
         self.ref = torch.zeros(n_pages, dtype=torch.int32, device=device)
         self.lens = torch.zeros(n_seqs, dtype=torch.int32, device=device)
         self.n_layers, self.page_size = n_layers, page_size
+        self._copies = False                      # whether `copy` is known to take these pools
+
+    def _check_copy(self):
+        """Refuses what `copy` would refuse, before a table changes."""
+        _detached(self.k, self.v)
+        if not self._copies:
+            none = self.lens[:0]
+            copy(self.k, self.v, none, none)
+            self._copies = True
 
     def reserve(self, n_new):
         """Room for n_new [n_seqs] tokens, shared pages copied: the Reserved."""
+        self._check_copy()
         got = reserve(self.table, self.ref, self.lens, n_new, self.page_size)
         copy(self.k, self.v, got.src, got.dst, got.state, got.tokens)
         return got
@@ -438,6 +447,7 @@ class PagedCache:
 
     def compact(self):
         """Moves the pages in use to the front: the Compacted."""
+        self._check_copy()
         got = compact(self.table, self.ref)
         copy(self.k, self.v, got.src, got.dst, got.state)
         return got
