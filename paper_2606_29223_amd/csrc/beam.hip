@@ -25,6 +25,7 @@ constexpr int LIST = 252;                 // candidates a wave sorts
 constexpr int LIST_ROOM = LIST + 4;
 constexpr int JOIN_WAVES = 8;
 constexpr int HOLD = 32;                  // lanes whose logits go through LDS
+constexpr int HELD = 8;                   // candidates a lane of the join keeps; further ones are read twice
 
 struct Cand {
   uint32_t key;                           // order-preserving bits of the logit; 0: none
@@ -322,7 +323,6 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void beam_join_kernel(BeamArgs a, 
     bool dead = !(score > -INFINITY && score < INFINITY);
     const Cand *c = cand + (size_t)row * n_seg * n;
     const int all = n_seg * n;
-    constexpr int HELD = 8;                       // candidates a lane keeps; further ones are read twice
     Cand held[HELD];
     uint32_t best = 0;
     double lse = 0.0;
@@ -439,22 +439,24 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void beam_join_kernel(BeamArgs a, 
 }  // namespace
 
 // Logits of a lane: 32, or 8 where that leaves the join of a row one segment a
-// lane and the GPU's 1024 SIMDs at most a wave each, so that a call is one wave's
-// time. 8 against 32, bf16, us: 4 rows of 8000 logits 8.7 / 10.1, of 32000 9.0 /
-// 9.6, 16 rows of 32000 12.7 / 13.1; past either limit 8 rows of 65000 16.5 /
-// 13.2, 64 rows of 32000 13.9 / 13.4, 512 rows 28.1 / 22.5.
-static int lane_logits(int rows, int vocab) {
+// lane and no more candidates than its lanes hold, and the GPU's 1024 SIMDs at
+// most a wave each, so that a call is one wave's time.  8 against 32, bf16, us: 4 rows of 8000 logits 8.7 /
+// 9.7, of 32000 8.9 / 9.6, 16 rows of 32000 in requests of eight 12.4 / 12.7; past
+// a limit 8 rows of 65000 16.6 / 13.0, 64 rows of 32000 13.9 / 13.1, 512 rows 28.9
+// / 22.0; more candidates: 12 beams of 32000 20.6 / 16.9, 16 44.8 / 23.9, 4 beams
+// and 64 candidates 874 / 290.
+static int lane_logits(int rows, int vocab, int n_out) {
   const int n_seg = segments(vocab, 64 * 8);
-  return n_seg <= 64 && (int64_t)rows * n_seg <= 1024 ? 8 : 32;
+  return n_seg <= 64 && n_out <= HELD && (int64_t)rows * n_seg <= 1024 ? 8 : 32;
 }
 
 size_t beam_work(int rows, int vocab, int n_out) {
-  const size_t n_seg = segments(vocab, 64 * lane_logits(rows, vocab));
+  const size_t n_seg = segments(vocab, 64 * lane_logits(rows, vocab, n_out));
   return (size_t)rows * n_seg * (n_out * sizeof(Cand) + sizeof(SegStat));
 }
 
 hipError_t launch_beam(int dtype, const BeamArgs &a, hipStream_t s) {
-  const int rows = a.requests * a.beams, lane = lane_logits(rows, a.vocab);
+  const int rows = a.requests * a.beams, lane = lane_logits(rows, a.vocab, a.n_out);
   const int n_seg = segments(a.vocab, 64 * lane);
   Cand *cand = (Cand *)a.work;
   SegStat *stat = (SegStat *)(cand + (size_t)rows * n_seg * a.n_out);
