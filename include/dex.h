@@ -423,8 +423,8 @@ dex_status dex_rotary_turns(int32_t scaling, int32_t rot_dim, double theta, doub
  * at row * row_stride + h * head_stride + d of its array, strides in elements
  * of dtype.  An output may be its input with the same strides, or memory that
  * overlaps no input.  inverse: turns back, R(-pos), which is also the
- * rotation's gradient.  Positions are any int32; the angle is formed in
- * double.  n_rows * head_dim * (n_heads + n_kv_heads + 8) < 2^35.            */
+ * rotation's gradient (scaled by `amplitude` again, so the two undo each other
+ * where that is 1).  Positions are any int32; the angle is formed in double.  n_rows * head_dim * (n_heads + n_kv_heads + 8) < 2^35.            */
 dex_status dex_rope(int32_t dtype, int32_t head_dim, const dex_rotary *rotary, int32_t inverse, int32_t n_rows,
                     const int32_t *pos, const void *q, int64_t q_row, int64_t q_head, int32_t n_heads, void *q_out,
                     int64_t q_out_row, int64_t q_out_head, const void *k, int64_t k_row, int64_t k_head,
@@ -454,12 +454,15 @@ dex_status dex_pages_append(int32_t dtype, int32_t head_dim, const dex_rotary *r
  *   lse = m + ln sum_j e^(s_j - m)   (float [n_rows][n_heads], or NULL).
  * A row that sees no key (row_len <= 0, a sequence outside [0, n_seqs), no
  * page) gets zeros and -inf.  No row_len exceeds max_len, which sizes the
- * work: keys past it, or past the table, are not attended to.  head_dim 32,
- * 64 or 128; n_heads a multiple of n_kv_heads, at most 64 times it and 8192; q, out and
- * the cache are of dtype, sums and statistics float.  Consecutive `group` rows
- * whose leading pages are the same (the beams of a request) have those read
- * once for all of them; any group gives the same bits.  A row's bits depend on
- * its own keys and query alone.                                             */
+ * work: a longer one counts as max_len, or as the table's width, for its window
+ * too.  head_dim 32, 64 or 128; n_heads a multiple of n_kv_heads, at most 64
+ * times it and 8192; q, out and the cache are of dtype, sums, weights and
+ * statistics float.  Consecutive `group` rows whose leading pages are the same
+ * (the beams of a request) have those read once for several of them: for 32 /
+ * (n_heads / n_kv_heads) rows at a time, all of them with keys and with the same
+ * first key, in whole steps of 256 keys, 512 past 6144 keys, 1024 past 12288 and
+ * so on, the same for all (rows on both sides of such a length share nothing).
+ * Any group gives the same bits: a row's depend on its own keys and query alone. */
 int64_t dex_pages_attention_work(int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                  int32_t max_len, int32_t group);
 dex_status dex_pages_attention(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads, int32_t n_rows,
@@ -490,7 +493,9 @@ dex_status dex_pages_fork(const int32_t *table, const int32_t *ref, const int32_
  * last page that others hold too is replaced by one of the sequence's own, and
  * (src, dst, tokens) says what dex_pages_copy has to copy before the next
  * write: its first `tokens` slots.  The last of several writers keeps the page
- * if no one else holds it.  Writes
+ * if no one else holds it.  Where that page is not there the sequence gets one
+ * whose first slots hold whatever they held.  ref has to count every table row
+ * that lists a page: one with count 0 is given out again.  Writes
  *   table, ref, length   updated (length[s] += n_new[s]);
  *   pos[s]     the first new position, or -1 (nothing asked, or not granted);
  *   src, dst, tokens     int32 [n_seqs], the copies first, then -1, -1, 0;
@@ -528,7 +533,10 @@ dex_status dex_pages_copy(int32_t dtype, int32_t head_dim, int32_t n_layers, int
  * largest total, largest first, equal ones by beam and token: parent (row
  * request * beams + beam, as dex_pages_fork takes it), token, score (the
  * total), done (the beam's, or token == eos; NULL: not wanted).  Within a beam
- * candidates are compared by their logits, across beams in double.  logits:
+ * candidates are compared by their logits, across beams by totals in double,
+ * whose lse is off by at most (9 + 2 E) 2^-24 (E the mean of maximum - logit
+ * under the softmax; a few 2^-26 as a rule) and is the same for beams of the
+ * same logits, so that these tie.  logits:
  * [requests * beams][vocab] of dtype, rows ld elements apart, any alignment.
  * beams and n_out 1 .. 64, n_out <= beams * vocab, requests * beams <= 2^20,
  * requests * beams * (vocab / 2048 + 2) <= 2^25; eos in [0, vocab), or -1 (with

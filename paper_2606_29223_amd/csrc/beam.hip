@@ -155,7 +155,7 @@ __device__ __forceinline__ uint4 load_grain(const T *p) {
 // What bounds it is the instructions: a logit takes a conversion, the maximum,
 // the exponential's five and one comparison with the threshold below, a wave
 // about 200 more.  320 rows of 65537 bf16 logits (42 MB, 8 us at a copy's rate)
-// take 18 us; 4 rows of 32000 floats 3.9 us, the latency of one wave.
+// take 18 us; 4 rows of 32000 floats 3.8 us, the latency of one wave.
 template <typename T, int LANE>
 __global__ __launch_bounds__(WAVES * 64, 5) void beam_segment_kernel(BeamArgs a, int n_seg, Cand *cand, SegStat *stat) {
   constexpr int GR = kGrain<T>, IT = LANE / GR, SEG = 64 * LANE;
@@ -303,8 +303,13 @@ __global__ __launch_bounds__(WAVES * 64, 5) void beam_segment_kernel(BeamArgs a,
 }
 
 // One workgroup a request, a wave a beam at a time, then all beams together:
-// the latency of a few dependent loads and of the double logarithm (5.2 us for
-// one request, 8.4 for 64 of eight beams).
+// the latency of a few dependent loads and of the double logarithm (5.3 us for
+// one request, 8.3 for 64 of eight beams) while few candidates reach the
+// threshold.  Where most do they are ranked in LDS, and more than LIST are taken
+// one by one in n passes over all: where fewer than n tokens of a large vocabulary
+// are allowed, the rest being equal at -inf (one token, the whole call: 64 x 8 x
+// 65537 51 us for 31, 4 x 32000 fp32 50 for 8.8), and with many beams (16 of 32000
+// 24 us, 64 of 4000 490).
 __global__ __launch_bounds__(JOIN_WAVES * 64) void beam_join_kernel(BeamArgs a, int n_seg, const Cand *cand,
                                                                    const SegStat *stat) {
   extern __shared__ double shared[];
@@ -440,11 +445,11 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void beam_join_kernel(BeamArgs a, 
 
 // Logits of a lane: 32, or 8 where that leaves the join of a row one segment a
 // lane and no more candidates than its lanes hold, and the GPU's 1024 SIMDs at
-// most a wave each, so that a call is one wave's time.  8 against 32, bf16, us: 4 rows of 8000 logits 8.7 /
-// 9.7, of 32000 8.9 / 9.6, 16 rows of 32000 in requests of eight 12.4 / 12.7; past
-// a limit 8 rows of 65000 16.6 / 13.0, 64 rows of 32000 13.9 / 13.1, 512 rows 28.9
-// / 22.0; more candidates: 12 beams of 32000 20.6 / 16.9, 16 44.8 / 23.9, 4 beams
-// and 64 candidates 874 / 290.
+// most a wave each, so that a call is one wave's time.  8 against 32, bf16, us: 4
+// rows of 8000 logits 8.7 / 9.7, of 32000 8.9 / 9.6, 16 rows of 32000 in requests
+// of eight 12.4 / 12.7; past a limit 8 rows of 65000 16.6 / 13.0, 64 rows of 32000
+// 13.9 / 13.1, 512 rows 28.9 / 22.0; more candidates: 12 beams of 32000 20.6 /
+// 16.9, 16 44.8 / 23.9, 4 beams and 64 candidates 874 / 290.
 static int lane_logits(int rows, int vocab, int n_out) {
   const int n_seg = segments(vocab, 64 * 8);
   return n_seg <= 64 && n_out <= HELD && (int64_t)rows * n_seg <= 1024 ? 8 : 32;

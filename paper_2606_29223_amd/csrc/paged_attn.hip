@@ -20,12 +20,14 @@
 // bits, so that weights are as exact as in fp32: against two parts (2^-17) it
 // costs 0 to 3 % (16 x 2000 keys 37.5 and 38.2 us, 8 x 8300 62.6 and 62.5).
 //
-// Measured (32 / 8 heads of 128, bf16): 8 rows of 8300 keys 56.8 us and the join
-// 4.7 for 272 MB, 4.8 TB/s in the kernel; 64 rows of 1 to 16000 keys 99 + 4.9
-// (461 MB); the loads alone, without products, take as long (392 of 399 us at 64
-// x 8000).  A single short row is the latency of the chain length, table, keys,
-// products, join: 9.2 + 3.3 us at 700 keys.  Splits: with 32 a row the records
-// cost 64 x 8000 keys 5 %, with 16 one long row lost 8 %.
+// Measured (32 / 8 heads of 128, bf16): 8 rows of 8300 keys 58.8 us and the join
+// 4.8 for 272 MB, 4.6 TB/s in the kernel; 64 rows of 1 to 16000 keys 100 + 5.1
+// (461 MB); the loads alone, without products, take as long (392 of 395 us at 64
+// x 8000).  Items go to the workgroups in turn whatever their size, and the most
+// loaded one has 1.5 and 1.4 to 1.7 times the mean's keys there.  A single short
+// row is the latency of the chain length, table, keys, products, join: 9.3 + 3.5
+// us at 700 keys.  Splits: with 32 a row the records cost 64 x 8000 keys 5 %,
+// with 16 one long row lost 8 %.
 #include "attn_decode.h"
 #include "dex.h"
 #include "paged.h"
@@ -434,8 +436,9 @@ __device__ __forceinline__ int group_rows(const Sharing &g, int r, int n_rows) {
 
 // The leading splits that are the same keys for every row of a group: one
 // workgroup compares their table rows (6 us; 16 x 8 rows that share 4000 of 4090
-// keys then take 84 + 8.5 us, alone 261 + 32).  They are the same work only where all
-// rows are cut alike and see all of the split, or all have one length.
+// keys then take 99 us in all, alone 249).  They are the same work only where all
+// rows are cut alike and see all of the split, or all have one length; one row
+// that is not (an empty one, one of another shift) leaves each to itself.
 __global__ __launch_bounds__(PA_THREADS) void paged_share_kernel(PagedAttnArgs a, Sharing g, int *share) {
   __shared__ int lens[PA_COLS], seqs[PA_COLS], first;
   const int tid = threadIdx.x, parts = (g.group + g.rows - 1) / g.rows;

@@ -235,7 +235,8 @@ def attention(q, k_pages, v_pages, table, lens, seq=None, max_len=None, scale=No
     first lens[r] keys of sequence seq[r] (r without `seq`), the last `window`
     of them if that is not 0.  `max_len` bounds lens (the table's width
     otherwise): the tighter, the less work memory.  group: so many
-    consecutive rows may share leading pages, which are then read once.
+    consecutive rows may share leading pages, which are then read once (of
+    rows that have keys and begin at the same key; dex.h has the steps).
     Returns out, or (out, lse); a row without keys gets 0 and -inf."""
     _detached(q, k_pages, v_pages, out)
     d, (n_pages, kv, ps, hd) = _pages(k_pages, v_pages, table)
