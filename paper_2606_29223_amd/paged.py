@@ -368,8 +368,9 @@ def copy(k_pool, v_pool, src, dst, count=None, tokens=None):
         if count.dim() != 1 or count.shape[0] < 1:
             _refuse("count holds the number of entries in its first element")
         num = _ints(count, dev, count.shape, "count")
-    _run(dexlib.load().dex_pages_copy, dev, d, hd, layers, n_pages, kv, ps, k_pool.data_ptr(), v_pool.data_ptr(), s, t,
-         tok, num, n)
+    if n > 0:
+        _run(dexlib.load().dex_pages_copy, dev, d, hd, layers, n_pages, kv, ps, k_pool.data_ptr(), v_pool.data_ptr(), s, t,
+             tok, num, n)
 
 
 def beam_select(logits, scores, n_out=None, done=None, eos=-1):
@@ -422,9 +423,10 @@ class PagedCache:
     def _check_copy(self):
         """Refuses what `copy` would refuse, before a table changes."""
         _detached(self.k, self.v)
-        if not self._copies:
-            none = self.lens[:0]
-            copy(self.k, self.v, none, none)
+        if not self._copies:                      # of no entries: the sizes are looked at, nothing is launched
+            layers, n_pages, kv, ps, hd = self.k.shape
+            _run(dexlib.load().dex_pages_copy, self.k.device, _gpu(self.k, "k"), hd, layers, n_pages, kv, ps,
+                 self.k.data_ptr(), self.v.data_ptr(), None, None, None, None, 0)
             self._copies = True
 
     def reserve(self, n_new):

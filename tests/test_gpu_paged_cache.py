@@ -53,3 +53,5 @@ def test_no_entries_are_no_copy():
     was, none = c.k.clone(), torch.empty(0, dtype=torch.int32, device="cuda")
     paged.copy(c.k, c.v, none, none)
     assert torch.equal(c.k, was)
+    odd = torch.zeros((1, 2, 1, 4, 3), device="cuda")      # rows that a copy would refuse
+    assert paged.copy(odd, odd, none, none) is None
