@@ -424,7 +424,8 @@ dex_status dex_rotary_turns(int32_t scaling, int32_t rot_dim, double theta, doub
  * of dtype.  An output may be its input with the same strides, or memory that
  * overlaps no input.  inverse: turns back, R(-pos), which is also the
  * rotation's gradient (scaled by `amplitude` again, so the two undo each other
- * where that is 1).  Positions are any int32; the angle is formed in double.  n_rows * head_dim * (n_heads + n_kv_heads + 8) < 2^35.            */
+ * where that is 1).  Positions are any int32; the angle is formed in double.
+ * n_rows * head_dim * (n_heads + n_kv_heads + 8) < 2^35.                     */
 dex_status dex_rope(int32_t dtype, int32_t head_dim, const dex_rotary *rotary, int32_t inverse, int32_t n_rows,
                     const int32_t *pos, const void *q, int64_t q_row, int64_t q_head, int32_t n_heads, void *q_out,
                     int64_t q_out_row, int64_t q_out_head, const void *k, int64_t k_row, int64_t k_head,
@@ -462,7 +463,8 @@ dex_status dex_pages_append(int32_t dtype, int32_t head_dim, const dex_rotary *r
  * (n_heads / n_kv_heads) rows at a time, all of them with keys and with the same
  * first key, in whole steps of 256 keys, 512 past 6144 keys, 1024 past 12288 and
  * so on, the same for all (rows on both sides of such a length share nothing).
- * Any group gives the same bits: a row's depend on its own keys and query alone. */
+ * Any group gives the same bits: a row's depend on its own keys and query
+ * alone.                                                                    */
 int64_t dex_pages_attention_work(int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                  int32_t max_len, int32_t group);
 dex_status dex_pages_attention(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads, int32_t n_rows,
@@ -536,11 +538,10 @@ dex_status dex_pages_copy(int32_t dtype, int32_t head_dim, int32_t n_layers, int
  * candidates are compared by their logits, across beams by totals in double,
  * whose lse is off by at most (9 + 2 E) 2^-24 (E the mean of maximum - logit
  * under the softmax; a few 2^-26 as a rule) and is the same for beams of the
- * same logits, so that these tie.  logits:
- * [requests * beams][vocab] of dtype, rows ld elements apart, any alignment.
- * beams and n_out 1 .. 64, n_out <= beams * vocab, requests * beams <= 2^20,
- * requests * beams * (vocab / 2048 + 2) <= 2^25; eos in [0, vocab), or -1 (with
- * done NULL): none.                                                         */
+ * same logits, so that these tie.  logits: [requests * beams][vocab] of dtype,
+ * rows ld elements apart, any alignment.  beams and n_out 1 .. 64, n_out <=
+ * beams * vocab, requests * beams <= 2^20, requests * beams * (vocab / 2048 + 2)
+ * <= 2^25; eos in [0, vocab), or -1 (with done NULL): none.                  */
 int64_t dex_beam_select_work(int32_t dtype, int32_t requests, int32_t beams, int32_t vocab, int32_t n_out);
 dex_status dex_beam_select(int32_t dtype, const void *logits, int64_t ld, int32_t requests, int32_t beams,
                            int32_t vocab, const float *score, const uint8_t *done, int32_t eos, int32_t n_out,
