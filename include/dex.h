@@ -548,6 +548,136 @@ dex_status dex_beam_select(int32_t dtype, const void *logits, int64_t ld, int32_
                            int32_t *parent, int32_t *token, float *score_out, uint8_t *done_out, void *work,
                            void *hip_stream);
 
+/* ---------------------------------------------------------------------------
+ * Over the same cache: trees of drafted tokens, attention over chosen pages,
+ * and eviction by accumulated attention weight.  What is said above of arrays,
+ * streams, work memory and refusals holds here too.  head_dim of the attention
+ * calls and of bounds and selection is 32, 64 or 128, n_heads a multiple of
+ * n_kv_heads, at most 64 times it and 8192, rows * n_heads <= 2^30.
+ * ------------------------------------------------------------------------- */
+
+/* Trees.  Node i < draft (1 to 256) of tree b is a drafted token, parent[b][i]
+ * the node it continues: a number in [0, i), anything else makes it a root.
+ * mask[b][i] (uint64 [ceil(draft / 64)]): bit j is set if j is node i or one of
+ * its ancestors.  depth[b][i] (or NULL): how many ancestors it has.            */
+dex_status dex_tree_mask(const int32_t *parent, int32_t n_trees, int32_t draft, uint64_t *mask, int32_t *depth,
+                         void *hip_stream);
+
+/* Which path of a tree the model agrees with: a node is accepted if its parent
+ * is and its token is target[b][parent], what the model wants there; a root, if
+ * its token is root[b] (root NULL: always).  Nodes from n_draft[b] on (NULL:
+ * draft) are none.  path[b] lists the nodes from a root to the deepest accepted
+ * one, the lowest number of equally deep ones, then -1; count[b] is their
+ * number, next[b] the target of the last, root[b] (or -1) if there is none.   */
+dex_status dex_tree_accept(const int32_t *parent, const int32_t *token, const int32_t *target, const int32_t *n_draft,
+                           const int32_t *root, int32_t n_trees, int32_t draft, int32_t *path, int32_t *count,
+                           int32_t *next, void *hip_stream);
+
+/* Attention of the drafted tokens of trees over one layer.  Row b * draft + i is
+ * node i of tree b, of sequence tree_seq[b] (NULL: b) with tree_len[b] keys
+ * before the tree (a longer one counts as max_len, below 0 as 0); node j's key
+ * and value are at position tree_len[b] + j (dex_pages_append puts them there;
+ * its rotary position is tree_len[b] + depth, so turn it with dex_rope first).
+ * The row sees the keys before the tree, and node j's if bit j of mask[b][i] is
+ * set, j < tree_draft[b] (NULL: draft), each only where its page is there; the
+ * mask may be any, and what it hides has no effect, NaN and infinity neither.
+ * Softmax, out and lse as dex_pages_attention's; a row that sees nothing, and
+ * the rows from tree_draft[b] on, get zeros and -inf.                         */
+int64_t dex_pages_tree_attention_work(int32_t dtype, int32_t n_trees, int32_t draft, int32_t n_heads, int32_t n_kv_heads,
+                                      int32_t head_dim, int32_t max_len);
+dex_status dex_pages_tree_attention(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads, int32_t n_trees,
+                                    int32_t draft, const int32_t *tree_seq, const int32_t *tree_len,
+                                    const int32_t *tree_draft, int32_t max_len, float scale, const void *q, int64_t q_row,
+                                    int64_t q_head, const uint64_t *mask, const void *k_pages, const void *v_pages,
+                                    int32_t n_pages, int32_t page_size, const int32_t *table, int32_t n_seqs,
+                                    int32_t max_pages, void *out, int64_t out_row, int64_t out_head, float *lse,
+                                    void *work, void *hip_stream);
+
+/* Moves tokens inside their sequences, in every layer of a pool: for j <
+ * min(count[s], capacity), position first[s] + j (first NULL: 0) of sequence s
+ * receives keys and values of its position first[s] + index[j], where index is
+ * at index + layer * index_layer + s * index_seq + head * index_head (strides in
+ * elements, 0 for what shares a list).  to_table NULL: in place, and an entry
+ * with index[j] <= j copies nothing (index[j] = j is there already); otherwise
+ * into the pages of to_table [n_seqs][to_pages], which the call does not read.
+ * An entry below 0, or without a page on either side, copies nothing.  All reads
+ * are of the old contents.  A page written to has no other holder, in the call's
+ * table or out of it.  A head's row is a multiple of 16 bytes.                */
+dex_status dex_pages_keep(int32_t dtype, int32_t head_dim, int32_t n_layers, int32_t n_pages, int32_t n_kv_heads,
+                          int32_t page_size, void *k_pool, void *v_pool, const int32_t *table, int32_t n_seqs,
+                          int32_t max_pages, const int32_t *to_table, int32_t to_pages, const int32_t *first,
+                          const int32_t *index, int64_t index_layer, int64_t index_seq, int64_t index_head,
+                          int32_t capacity, const int32_t *count, void *hip_stream);
+
+/* Pages behind a sequence's last token (length[s]; below 0 counts as 0) leave its
+ * row of the table, whose entries there become -1, and lose a holder.  table_out
+ * and ref_out may be their inputs.                                            */
+dex_status dex_pages_trim(const int32_t *table, const int32_t *ref, const int32_t *length, int32_t n_seqs,
+                          int32_t max_pages, int32_t n_pages, int32_t page_size, int32_t *table_out, int32_t *ref_out,
+                          void *hip_stream);
+
+/* Bounds of the keys of a page: bounds[p][h] (of dtype, [2][head_dim], 16-byte
+ * aligned) is the least and the largest of its keys in every dimension, over the
+ * tokens before length[s]; a NaN is passed over, and NaN alone gives NaN.  Writes those of the pages that
+ * hold the last n_new tokens of each sequence (more than it has: all), the others
+ * stay.  Sequences that share such a page hold the same number of its tokens.  */
+dex_status dex_pages_bounds(int32_t dtype, int32_t head_dim, const void *k_pages, int32_t n_pages, int32_t n_kv_heads,
+                            int32_t page_size, const int32_t *table, int32_t n_seqs, int32_t max_pages,
+                            const int32_t *length, int32_t n_new, void *bounds, void *hip_stream);
+
+/* The pages to read for each row and kv head h: of the columns of its sequence's
+ * table that hold tokens (row_len as dex_pages_attention takes it) and a page,
+ * the first `sinks`, the last `recent`, and those of largest score
+ *   sum over h's query heads and dimensions of max(q_d least_d, q_d largest_d),
+ * of equal ones the first, up to n_select in all.  columns[r][h] [n_select]
+ * lists them ascending, then -1.  Scores are in double; a q_d of 0 adds 0, and a
+ * score that is NaN counts as infinity.                                       */
+int64_t dex_pages_select_work(int32_t n_rows, int32_t n_kv_heads, int32_t page_size, int32_t max_len);
+dex_status dex_pages_select(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads, int32_t n_rows,
+                            const int32_t *row_seq, const int32_t *row_len, int32_t max_len, const void *q, int64_t q_row,
+                            int64_t q_head, const void *bounds, int32_t n_pages, int32_t page_size, const int32_t *table,
+                            int32_t n_seqs, int32_t max_pages, int32_t n_select, int32_t sinks, int32_t recent,
+                            int32_t *columns, void *work, void *hip_stream);
+
+/* dex_pages_attention over the listed columns alone: row r's heads of kv head h
+ * see the tokens before row_len[r] of columns[r][h] [n_columns], in any order (a
+ * column listed twice counts twice; one outside the table is none).  Of a row
+ * only the first ceil(row_len / page_size) entries are read.                  */
+int64_t dex_pages_sparse_attention_work(int32_t dtype, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
+                                        int32_t head_dim, int32_t n_columns, int32_t page_size);
+dex_status dex_pages_sparse_attention(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads,
+                                      int32_t n_rows, const int32_t *row_seq, const int32_t *row_len, float scale,
+                                      const void *q, int64_t q_row, int64_t q_head, const int32_t *columns,
+                                      int32_t n_columns, const void *k_pages, const void *v_pages, int32_t n_pages,
+                                      int32_t page_size, const int32_t *table, int32_t n_seqs, int32_t max_pages,
+                                      void *out, int64_t out_row, int64_t out_head, float *lse, void *work,
+                                      void *hip_stream);
+
+/* dex_pages_attention of one new token a row that also adds up what each key was
+ * given: weight_out[r][h][j] = weight[r][h][j] + the sum of the softmax weights of
+ * key j over the query heads of kv head h, for j < row_len[r] (0 for a key whose
+ * page is not there); what lies behind stays.  Rows [n_rows][n_kv_heads] of float,
+ * weight_ld and weight_out_ld >= max_len elements apart; weight_out may be weight
+ * with the same stride.                                                       */
+int64_t dex_pages_weigh_work(int32_t dtype, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                             int32_t max_len);
+dex_status dex_pages_weigh(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads, int32_t n_rows,
+                           const int32_t *row_seq, const int32_t *row_len, int32_t max_len, float scale, const void *q,
+                           int64_t q_row, int64_t q_head, const float *weight, int64_t weight_ld, float *weight_out,
+                           int64_t weight_out_ld, const void *k_pages, const void *v_pages, int32_t n_pages,
+                           int32_t page_size, const int32_t *table, int32_t n_seqs, int32_t max_pages, void *out,
+                           int64_t out_row, int64_t out_head, float *lse, void *work, void *hip_stream);
+
+/* Which keys of each sequence and kv head stay: the first `sinks`, the last
+ * `recent`, and the heaviest others (of equal ones the first; a NaN counts as
+ * infinity), count[s] = min(length[s], capacity, budget) in all.  index[s][h]
+ * [budget] lists them ascending, then -1, as dex_pages_keep takes it;
+ * weight_out[s][h] [capacity] is their weights in that order, then 0.  weight_out
+ * may be weight with the same stride.                                         */
+dex_status dex_pages_evict(const float *weight, int64_t weight_ld, int32_t n_seqs, int32_t n_kv_heads, int32_t capacity,
+                           const int32_t *length, int32_t budget, int32_t sinks, int32_t recent, int32_t *index,
+                           int32_t *count, float *weight_out, int64_t weight_out_ld, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

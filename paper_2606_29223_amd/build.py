@@ -19,7 +19,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libdex.so")
 
 SOURCES = ["gemm.hip", "gemm_prefill.hip", "attn.hip", "misc.hip", "rope.hip", "pages.hip", "paged_attn.hip", "beam.hip",
-           "engine.cpp", "paged.cpp"]
+           "span_attn.hip", "tree.hip", "select.hip", "engine.cpp", "paged.cpp", "span.cpp"]
 ARCH = "gfx950"
 
 HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"

@@ -1,0 +1,810 @@
+// Attention of the rows of a sequence that share its keys: a tree of drafted
+// tokens, or one row over chosen pages, or one row whose softmax weights are
+// kept.
+//
+// Row i of a sequence with L keys sees the keys j < L whose page is there and,
+// of the drafted keys L + t, those with bit t of its mask: s_j = scale q.k_j,
+// out = sum e^{s_j - m} v_j / sum e^{s_j - m}, lse = m + ln sum e^{s_j - m}.
+#include "attn_decode.h"
+#include "dex.h"
+#include "span.h"
+
+#include <algorithm>
+
+namespace dex {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// What keys that no row sees are read from: a row of zeros.
+__device__ uint4 zero_row[32];
+
+// How the keys of a sequence are cut: `n` splits of `steps` steps, a step being
+// a tile for each of a workgroup's key groups.
+struct SpanPlan {
+  int steps, n;
+};
+__host__ __device__ __forceinline__ SpanPlan span_plan(int keys, int step_keys, int smax, int least) {
+  const int all = (keys + step_keys - 1) / step_keys;
+  SpanPlan p;
+  p.steps = max(least, (all + smax - 1) / smax);
+  p.n = max(1, (all + p.steps - 1) / p.steps);
+  return p;
+}
+
+// What a launch of a case is told beside its arguments.
+struct SpanGrid {
+  int blocks;                             // column blocks of a (sequence, kv head)
+  int smax, least;                        // splits at most, steps of a split at least
+  float *rec;                             // [n * draft][n_heads][smax][head_dim]
+  float2 *stat;                           // [n * draft][n_heads][smax]: maximum, sum
+  float *score;                           // [n][n_heads][score_ld], or null
+  int64_t score_ld;
+  bool whole;                             // queries and outputs lie on 16-byte boundaries
+};
+
+// The sequence's own numbers: keys before the drafted ones, drafted ones, and
+// the places that are looked at (all keys, or those of the listed columns).
+struct Span {
+  int seq, len, drafted, keys;
+};
+__device__ __forceinline__ Span span_of(const SpanArgs &a, int i) {
+  Span s;
+  s.seq = a.seq != nullptr ? a.seq[i] : i;
+  const bool is = s.seq >= 0 && s.seq < a.map.n_seqs;
+  s.len = is ? max(0, min(min(a.len[i], a.max_len), a.map.max_pages << a.map.shift)) : 0;
+  s.drafted = 0;
+  if (a.mask != nullptr && is) s.drafted = a.n_draft != nullptr ? max(0, min(a.n_draft[i], a.draft)) : a.draft;
+  s.keys = s.len + s.drafted;
+  if (a.columns != nullptr) s.keys = min(a.n_cols, (s.len + (1 << a.map.shift) - 1) >> a.map.shift) << a.map.shift;
+  return s;
+}
+
+// Max over the four lanes r16, r16 + 16, + 32, + 48.
+__device__ __forceinline__ float quarters_max(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float quarters_sum(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+// A float's upper half is a bf16, and what is left of its 24 bits after that two
+// more: three parts that are the float, with no rounding.  Where nothing is left
+// a part is 2^-100, not 0, so that an infinite value times its weight, the sum
+// over the parts, is infinite (0 and negative parts would make it NaN).
+__device__ __forceinline__ uint32_t upper_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ float after_upper(float a) {
+  return fmaxf(a - __uint_as_float(__float_as_uint(a) & 0xffff0000u), 0x1p-100f);
+}
+
+// A tile of keys or values in LDS: TK rows of HD elements, whose 16-byte chunks
+// are swapped within a row (chunk c lies at c ^ swizzle) so that the 16 rows of
+// a key fragment, and the rows that half a wave reads of the values, lie in
+// different banks.  Filled by direct transfers of 1 KB, RPT rows each.
+template <typename T, int HD>
+struct Tile {
+  static constexpr int TK = sizeof(T) == 2 ? 32 : 16;
+  static constexpr int NT = TK / 16, DT = HD / 16;
+  static constexpr int RB = HD * sizeof(T), CPR = RB / 16, RPT = 64 / CPR, NTR = TK / RPT;
+  static constexpr int BYTES = TK * RB;
+  __device__ __forceinline__ static int kswz(int row) {
+    return CPR >= 16 ? (row & 15) : CPR == 8 ? ((row >> 1) & 7) : ((row >> 2) & 3);
+  }
+  __device__ __forceinline__ static int vswz(int row) {
+    if (sizeof(T) == 4) return 0;
+    return CPR == 16 ? 2 * (row & 7) : CPR == 8 ? 2 * ((row >> 1) & 3) : 2 * ((row >> 2) & 1);
+  }
+};
+
+// One wave's columns: 16 NB of them, column r16 of block nb; its scores and
+// outputs of them on the matrix cores.
+template <typename T, int HD, int NB>
+struct Cols;
+
+template <int HD, int NB>
+struct Cols<uint16_t, HD, NB> {
+  using L = Tile<uint16_t, HD>;
+  static constexpr int KS = HD / 32, NT = L::NT, DT = L::DT, CPR = L::CPR;
+  pf_bf16x8 q[NB][KS];
+  pf_f32x4 o[NB][DT];
+
+  __device__ __forceinline__ void load_q(int nb, const uint16_t *src, bool whole, float scale) {
+    const int grp = (threadIdx.x & 63) >> 4;
+    const uint32_t sign = scale < 0.f ? 0x80008000u : 0u, some = scale != 0.f ? ~0u : 0u;
+#pragma unroll
+    for (int st = 0; st < KS; ++st) {
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (src != nullptr) {
+        if (whole) {
+          x = *(const uint4 *)(src + st * 32 + grp * 8);
+        } else {
+          uint16_t e[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) e[i] = src[st * 32 + grp * 8 + i];
+          __builtin_memcpy(&x, e, 16);
+        }
+      }
+      q[nb][st] = __builtin_bit_cast(pf_bf16x8, make_uint4((x.x ^ sign) & some, (x.y ^ sign) & some, (x.z ^ sign) & some, (x.w ^ sign) & some));
+    }
+  }
+  __device__ __forceinline__ void scores(int used, const uint4 *k, pf_f32x4 (&sc)[NB][NT]) const {
+    const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) sc[nb][nt] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = 0; st < KS; ++st)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int row = nt * 16 + r16;
+        const pf_bf16x8 kf = __builtin_bit_cast(pf_bf16x8, k[row * CPR + ((st * 4 + grp) ^ L::kswz(row))]);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          if (nb < used) sc[nb][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[nb][st], sc[nb][nt], 0, 0, 0);
+      }
+  }
+  // o += V^T P^T; ODD: without the values that are no finite numbers
+  template <bool ODD>
+  __device__ __forceinline__ void outputs(int used, const uint4 *v, const pf_f32x4 (&p)[NB][NT]) {
+    const int lane = threadIdx.x & 63, tq = lane >> 4, ti = (lane & 15) >> 2, tg = lane & 3;
+    pf_bf16x8 pp[NB][3];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      uint32_t part[3][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a = p[nb][i / 2][2 * (i % 2)], b = p[nb][i / 2][2 * (i % 2) + 1];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          part[k][i] = upper_halves(a, b);
+          a = after_upper(a);
+          b = after_upper(b);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        pp[nb][k] = __builtin_bit_cast(pf_bf16x8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3]));
+    }
+    const uint16_t *base = (const uint16_t *)v;
+    const int lo = 4 * tq + ti, hi = lo + 16;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const int c = 2 * dt + (tg >> 1);
+      pf_bf16x8 vf = tr_frag(base + (lo * CPR + (c ^ L::vswz(lo))) * 8 + (tg & 1) * 4,
+                             base + (hi * CPR + (c ^ L::vswz(hi))) * 8 + (tg & 1) * 4);
+      if constexpr (ODD) {
+        uint4 x = __builtin_bit_cast(uint4, vf);
+        auto even = [](uint32_t w) {
+          if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+          return (w & 0x7f800000u) == 0x7f800000u ? w & 0xffffu : w;
+        };
+        vf = __builtin_bit_cast(pf_bf16x8, make_uint4(even(x.x), even(x.y), even(x.z), even(x.w)));
+      }
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          if (nb < used) o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[nb][k], o[nb][dt], 0, 0, 0);
+    }
+  }
+  // Element (key, d) of the values; whether a chunk of them holds one that is no finite number.
+  __device__ __forceinline__ static float value(const uint4 *v, int key, int d) {
+    const uint16_t *e = (const uint16_t *)v + (key * CPR + ((d / 8) ^ L::vswz(key))) * 8 + d % 8;
+    return __uint_as_float((uint32_t)*e << 16);
+  }
+  __device__ __forceinline__ static bool odd_chunk(const uint4 &x) {
+    auto odd = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
+    return odd(x.x) || odd(x.y) || odd(x.z) || odd(x.w);
+  }
+  // four neighbouring dimensions of an output: which, and their values
+  static constexpr int QUADS = DT;
+  __device__ __forceinline__ static int dim(int j) { return 16 * j + 4 * ((threadIdx.x & 63) >> 4); }
+  __device__ __forceinline__ pf_f32x4 quad(int nb, int j) const { return o[nb][j]; }
+  // dimension of o[.][dt][i]
+  __device__ __forceinline__ static int dim_of(int dt, int i) { return 16 * dt + 4 * ((threadIdx.x & 63) >> 4) + i; }
+};
+
+// fp32: a key lane holds dimensions 4 grp .. + 3 of each 16, so one 16-byte read
+// feeds four k-steps; a value lane holds W neighbouring dimensions of one key,
+// each the row of another 16-dimension tile.
+template <int HD, int NB>
+struct Cols<float, HD, NB> {
+  using L = Tile<float, HD>;
+  static constexpr int NT = L::NT, DT = L::DT, CPR = L::CPR, W = HD >= 64 ? 4 : 2, VB = HD / (16 * W);
+  typedef __attribute__((ext_vector_type(W))) float vecw;
+  pf_f32x4 q[NB][DT], o[NB][DT];
+
+  __device__ __forceinline__ void load_q(int nb, const float *src, bool whole, float scale) {
+    const int grp = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      pf_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+      if (src != nullptr) {
+        if (whole) {
+          x = *(const pf_f32x4 *)(src + t * 16 + grp * 4);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = src[t * 16 + grp * 4 + i];
+        }
+      }
+      q[nb][t] = scale < 0.f ? -x : scale != 0.f ? x : (pf_f32x4)0.f;
+    }
+  }
+  __device__ __forceinline__ void scores(int used, const uint4 *k, pf_f32x4 (&sc)[NB][NT]) const {
+    const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
+    // four sums of a quarter of the dimensions each: one sum of all rounds more
+    pf_f32x4 part[NB][4];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[nb][e] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const pf_f32x4 kf = __builtin_bit_cast(pf_f32x4, k[r16 * CPR + ((4 * t + grp) ^ L::kswz(r16))]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          if (nb < used) part[nb][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], q[nb][t][e], part[nb][e], 0, 0, 0);
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) sc[nb][0] = (part[nb][0] + part[nb][1]) + (part[nb][2] + part[nb][3]);
+  }
+  template <bool ODD>
+  __device__ __forceinline__ void outputs(int used, const uint4 *v, const pf_f32x4 (&p)[NB][NT]) {
+    const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = 4 * grp + i;
+      const float *row = (const float *)(v + key * CPR) + r16 * W;
+#pragma unroll
+      for (int b = 0; b < VB; ++b) {
+        vecw x = *(const vecw *)(row + b * 16 * W);
+        if constexpr (ODD) {
+#pragma unroll
+          for (int e = 0; e < W; ++e)
+            if ((__float_as_uint(x[e]) & 0x7f800000u) == 0x7f800000u) x[e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            if (nb < used)
+              o[nb][b * W + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], p[nb][0][i], o[nb][b * W + e], 0, 0, 0);
+      }
+    }
+  }
+  __device__ __forceinline__ static float value(const uint4 *v, int key, int d) {
+    return ((const float *)(v + key * CPR))[d];
+  }
+  __device__ __forceinline__ static bool odd_chunk(const uint4 &x) {
+    auto odd = [](uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; };
+    return odd(x.x) || odd(x.y) || odd(x.z) || odd(x.w);
+  }
+  static constexpr int QUADS = HD / 16;
+  __device__ __forceinline__ static int dim(int j) {
+    const int grp = (threadIdx.x & 63) >> 4;
+    return W == 4 ? 64 * (j / 4) + 16 * grp + 4 * (j % 4) : 8 * grp + 4 * j;
+  }
+  __device__ __forceinline__ pf_f32x4 quad(int nb, int j) const {
+    if constexpr (W == 4) {
+      const int b = 4 * (j / 4), i = j % 4;
+      return pf_f32x4{o[nb][b][i], o[nb][b + 1][i], o[nb][b + 2][i], o[nb][b + 3][i]};
+    } else {
+      return pf_f32x4{o[nb][0][2 * j], o[nb][1][2 * j], o[nb][0][2 * j + 1], o[nb][1][2 * j + 1]};
+    }
+  }
+  __device__ __forceinline__ static int dim_of(int dt, int i) {
+    return 16 * W * (dt / W) + W * (4 * ((threadIdx.x & 63) >> 4) + i) + dt % W;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void put(T *p, float v) {
+  if constexpr (sizeof(T) == 2) *p = __builtin_bit_cast(uint16_t, (__bf16)v);
+  else *p = v;
+}
+// What a sum over l is multiplied by: a NaN as it is, nothing as 0.
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l != l ? l : 0.f; }
+__device__ __forceinline__ float log_sum(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * kLn2; }
+
+// Four neighbouring dimensions of a row's output, and with the first its lse.
+template <typename T>
+__device__ __forceinline__ void finish(const SpanArgs &a, bool whole, int row, int head, int d, const pf_f32x4 &o, float m,
+                                       float l) {
+  const float inv = inverse(l);
+  T *out = (T *)a.out + (int64_t)row * a.out_row + (int64_t)head * a.out_head + d;
+  if (whole) {
+    rec_store4(out, o * inv);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put(out + i, o[i] * inv);
+  }
+  if (d == 0 && a.lse != nullptr) a.lse[(size_t)row * a.n_heads + head] = log_sum(m, l);
+}
+__device__ __forceinline__ size_t rec_index(const SpanArgs &a, int row, int head, int split, int smax) {
+  return ((size_t)row * a.n_heads + head) * smax + split;
+}
+
+// A wave's transfers are in LDS, but for the youngest N.
+template <int N>
+__device__ __forceinline__ void landed() {
+  static_assert(N >= 0 && N < 64, "vmcnt field");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+
+// The waves of a workgroup: WC neighbouring column blocks over the same keys,
+// WK = NW / WC groups of keys.
+template <typename T, int HD, int NB, int WC>
+struct Shape {
+  static constexpr int NW = WC > 4 ? WC : 4, WK = NW / WC, COLS = 16 * NB * WC;
+  using L = Tile<T, HD>;
+  static constexpr int STEP = L::TK * WK;                    // keys of a step
+  static constexpr int RING = 4 * L::BYTES;                  // a key group's two tiles of keys and values
+  static constexpr int MEET = WK > 1 ? NW * 16 * NB * (HD + 4) * 4 : 0;
+  static constexpr int LDS = RING * WK > MEET ? RING * WK : MEET;
+};
+
+template <typename T, int HD, int NB, int WC>
+__global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW)) void span_attn_kernel(SpanArgs a, SpanGrid g) {
+  using S = Shape<T, HD, NB, WC>;
+  using L = Tile<T, HD>;
+  using C = Cols<T, HD, NB>;
+  constexpr int TK = L::TK, NT = L::NT, NW = S::NW, WK = S::WK;
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+  __shared__ float wm[NW][16 * NB], wl[NW][16 * NB];
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wc = wave % WC, wk = wave / WC;
+  const int kv = a.map.n_kv_heads, G = a.n_heads / kv, cols = a.draft * G;
+  // kv heads innermost: with a multiple of eight of them the column blocks and
+  // neighbours of a head stay on one XCD
+  int x = blockIdx.x;
+  const int head = x % kv;
+  x /= kv;
+  const int block = x % g.blocks;
+  x /= g.blocks;
+  const int b = x % a.n, split = x / a.n;
+  const Span sp = span_of(a, b);
+  const SpanPlan plan = span_plan(sp.keys, S::STEP, g.smax, g.least);
+  if (split >= plan.n) return;
+  const int first = split * plan.steps * S::STEP;
+  const int steps = min(plan.steps, (sp.keys - first + S::STEP - 1) / S::STEP);
+  const int c0 = (block * WC + wc) * 16 * NB;                // the wave's first column
+  const int used = min(NB, (cols - c0 + 15) / 16);           // its blocks with columns
+  uint4 *ring = (uint4 *)(lds + wk * S::RING);
+
+  // the cache rows of a step's keys: lane j holds key j's
+  auto key_of = [&](int step) { return first + step * S::STEP + wk * TK; };
+  auto look = [&](int step) -> uint32_t {
+    if (step >= steps) return kNoRow;
+    const int slot = key_of(step) + (lane & (TK - 1));
+    if (slot >= sp.keys) return kNoRow;
+    int pos = slot;
+    if (a.columns != nullptr) {
+      const int c = a.columns[((size_t)b * kv + head) * a.n_cols + (slot >> a.map.shift)];
+      if (c < 0 || c >= a.map.max_pages) return kNoRow;
+      pos = (c << a.map.shift) + (slot & ((1 << a.map.shift) - 1));
+      if (pos >= sp.len) return kNoRow;
+    }
+    return page_row(a.map, sp.seq, pos, head);
+  };
+  // a step's keys and values into the ring: transfer c moves rows RPT c ..;
+  // lane l fills chunk l % CPR of row RPT c + l / CPR with the swizzled one
+  auto issue = [&](int step, uint32_t rows) {
+    uint4 *to = ring + (step & 1) * (2 * L::BYTES / 16);
+#pragma unroll
+    for (int t = 0; t < (L::NTR + WC - 1) / WC; ++t) {
+      const int c = t * WC + wc;
+      if (L::NTR % WC != 0 && c >= L::NTR) break;
+      const int row = c * L::RPT + lane / L::CPR, chunk = lane % L::CPR;
+      const uint32_t at = (uint32_t)__shfl((int)rows, row, 64);
+      const uint64_t off = (uint64_t)at * L::RB;
+      const char *kp = at == kNoRow ? (const char *)zero_row : (const char *)a.k + off;
+      const char *vp = at == kNoRow ? (const char *)zero_row : (const char *)a.v + off;
+      __builtin_amdgcn_global_load_lds((const void *)(kp + (chunk ^ L::kswz(row)) * 16),
+                                       (__attribute__((address_space(3))) void *)(to + c * 64), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const void *)(vp + (chunk ^ L::vswz(row)) * 16),
+                                       (__attribute__((address_space(3))) void *)(to + L::BYTES / 16 + c * 64), 16, 0, 0);
+    }
+  };
+
+  uint32_t rows = look(0), rows1 = look(1);
+  if (steps > 0) issue(0, rows);
+  C w;
+  float m[NB], l[NB];                     // reference (powers of two) and this lane's part of the sum
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int c = c0 + nb * 16 + r16;
+    const T *src = (const T *)a.q + ((int64_t)b * a.draft + c / G) * a.q_row + (int64_t)(head * G + c % G) * a.q_head;
+    w.load_q(nb, c < cols ? src : nullptr, g.whole, a.scale);
+    m[nb] = -INFINITY;
+    l[nb] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < C::DT; ++dt) w.o[nb][dt] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float scale2 = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;   // the query has the sign, or is 0
+
+  for (int step = 0; step < steps; ++step) {
+    const uint32_t rows2 = look(step + 2);
+    if constexpr (WC > 1) {
+      // the step has landed for every wave, and every wave is past the last
+      // one, whose place the next takes
+      lds_ring_step<0>();
+      if (step + 1 < steps) issue(step + 1, rows1);
+    } else {
+      if (step + 1 < steps) {
+        issue(step + 1, rows1);
+        landed<2 * L::NTR>();
+      } else {
+        landed<0>();
+      }
+    }
+    const uint4 *k = ring + (step & 1) * (2 * L::BYTES / 16), *v = k + L::BYTES / 16;
+    const int key0 = key_of(step);
+    const unsigned long long ballot = __ballot(lane < TK && rows != kNoRow);
+    const uint32_t there = (uint32_t)ballot;                 // keys that some row may see
+    constexpr uint32_t kAll = TK == 32 ? 0xffffffffu : 0xffffu;
+    const bool trees = a.mask != nullptr && key0 + TK > sp.len;
+    if (used > 0 && there != 0) {
+      pf_f32x4 sc[NB][NT];
+      w.scores(used, k, sc);
+      uint32_t sees[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) sees[nb] = there;
+      if (trees) {
+        // bit t of the row's mask is key len + t; keys before len are seen
+        const int d0 = key0 - sp.len, from = max(d0, 0);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const int c = min(c0 + nb * 16 + r16, cols - 1);
+          const uint64_t *bits = a.mask + ((size_t)b * a.draft + c / G) * a.words;
+          const int at = from >> 6, sh = from & 63;
+          uint64_t x = at < a.words ? bits[at] >> sh : 0;
+          if (sh > 0 && at + 1 < a.words) x |= bits[at + 1] << (64 - sh);
+          if (d0 < 0) x = x << -d0 | ((1ull << -d0) - 1);    // (-d0 < TK)
+          sees[nb] &= (uint32_t)x;
+        }
+      }
+      if (trees || there != kAll) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const uint32_t mine = sees[nb] >> (4 * grp);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (!(mine >> (nt * 16 + i) & 1)) sc[nb][nt][i] = -INFINITY;
+        }
+      }
+      if (g.score != nullptr) {
+        // (one row: a column is a head, and lies in block 0 .. NB - 1)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const int c = c0 + nb * 16 + r16;
+          if (c < cols) {
+            float *to = g.score + ((size_t)b * a.n_heads + head * G + c) * g.score_ld + key0 + 4 * grp;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) *(pf_f32x4 *)(to + 16 * nt) = sc[nb][nt] * scale2;
+          }
+        }
+      }
+      // A column's reference is raised, and its sums rescaled, only once a score
+      // exceeds it by 2^8, which leaves every rounding relative.
+      float mx[NB];
+      bool up = false;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float m0 = -INFINITY;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) m0 = fmaxf(m0, sc[nb][nt][i]);
+        mx[nb] = quarters_max(m0) * scale2;
+        up |= mx[nb] > m[nb] + 8.f;
+      }
+      if (__any(up)) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const float now = mx[nb] > m[nb] + 8.f ? mx[nb] : m[nb];
+          const float shrink = now == m[nb] ? 1.f : __builtin_amdgcn_exp2f(m[nb] - now);
+          m[nb] = now;
+          l[nb] *= shrink;
+#pragma unroll
+          for (int dt = 0; dt < C::DT; ++dt) w.o[nb][dt] *= shrink;
+        }
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const float ref = m[nb] == -INFINITY ? 0.f : -m[nb];
+        float sum = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(sc[nb][nt][i], scale2, ref));
+            sc[nb][nt][i] = p;
+            sum += p;
+          }
+        l[nb] += sum;
+      }
+      uint32_t bad = 0;
+      if (trees) {
+        // Drafted values that some rows see and others do not: 0 times an
+        // infinity or NaN is not 0, so those go by themselves.
+        for (int e = lane; e < TK * L::CPR; e += 64)
+          if (C::odd_chunk(v[e])) bad |= 1u << (e / L::CPR);
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) bad |= (uint32_t)__shfl_xor((int)bad, s, 64);
+        bad = (uint32_t)__builtin_amdgcn_readfirstlane((int)bad);
+      }
+      if (bad == 0) {
+        w.template outputs<false>(used, v, sc);
+      } else {
+        w.template outputs<true>(used, v, sc);
+        for (uint32_t left = bad; left != 0; left &= left - 1) {
+          const int key = __builtin_ctz(left);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            float p = 0.f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (key / 16 == nt && key % 4 == i) p = sc[nb][nt][i];
+            p = fmaxf(__shfl(p, (key >> 2 & 3) * 16 + r16, 64), 0x1p-100f);
+            if (sees[nb] >> key & 1) {
+#pragma unroll
+              for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const float x = C::value(v, key, C::dim_of(dt, i));
+                  if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) w.o[nb][dt][i] += p * x;
+                }
+            }
+          }
+        }
+      }
+    }
+    wave_lds_sync();                      // the tile is read before anything takes its place
+    rows = rows1;
+    rows1 = rows2;
+  }
+
+  // rows behind the drafted ones see nothing
+  auto give = [&](int c, int d, const pf_f32x4 &o, float mm, float ll) {
+    const int i = c / G, row = b * a.draft + i, hd = head * G + c - i * G;
+    const bool none = a.mask != nullptr && i >= sp.drafted;
+    const pf_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    if (plan.n == 1) {
+      finish<T>(a, g.whole, row, hd, d, none ? zero : o, none ? -INFINITY : mm, none ? 0.f : ll);
+      if (g.score == nullptr) return;
+    } else {
+      *(pf_f32x4 *)(g.rec + rec_index(a, row, hd, split, g.smax) * HD + d) = none ? zero : o;
+    }
+    if (d == 0) g.stat[rec_index(a, row, hd, split, g.smax)] = none ? make_float2(-INFINITY, 0.f) : make_float2(mm, ll);
+  };
+  if constexpr (WK == 1) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int c = c0 + nb * 16 + r16;
+      const float sum = quarters_sum(l[nb]);
+      if (c < cols) {
+#pragma unroll
+        for (int j = 0; j < C::QUADS; ++j) give(c, C::dim(j), w.quad(nb, j), m[nb], sum);
+      }
+    }
+  } else {
+    // the key groups' sums under one reference
+    typedef float Row[HD + 4];
+    __syncthreads();
+    Row *mine = (Row *)lds + wave * 16 * NB;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float sum = quarters_sum(l[nb]);
+      if (grp == 0) {
+        wm[wave][nb * 16 + r16] = m[nb];
+        wl[wave][nb * 16 + r16] = sum;
+      }
+#pragma unroll
+      for (int j = 0; j < C::QUADS; ++j) *(pf_f32x4 *)&mine[nb * 16 + r16][C::dim(j)] = w.quad(nb, j);
+    }
+    __syncthreads();
+    const int base = block * S::COLS, n = min(S::COLS, cols - base);
+    for (int e = tid; e < n * (HD / 4); e += 64 * NW) {
+      const int c = e / (HD / 4), d = e % (HD / 4) * 4, u = c / (16 * NB), at = c % (16 * NB);
+      float mm = wm[u][at];
+#pragma unroll
+      for (int s = 1; s < WK; ++s) mm = fmaxf(mm, wm[s * WC + u][at]);
+      const float ref = mm == -INFINITY ? 0.f : mm;
+      pf_f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      float ll = 0.f;
+#pragma unroll
+      for (int s = 0; s < WK; ++s) {
+        const float f = __builtin_amdgcn_exp2f(wm[s * WC + u][at] - ref);
+        const pf_f32x4 y = *(const pf_f32x4 *)&((const Row *)lds)[(s * WC + u) * 16 * NB + at][d];
+        ll = fmaf(f, wl[s * WC + u][at], ll);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(f, y[i], o[i]);
+      }
+      give(base + c, d, o, mm, ll);
+    }
+  }
+}
+
+// A row's records together, HD / 4 lanes a (row, query head).
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, SpanGrid g, int step_keys) {
+  constexpr int LPR = HD / 4, PER = 256 / LPR;
+  const int64_t id = (int64_t)blockIdx.x * PER + threadIdx.x / LPR;
+  if (id >= (int64_t)a.n * a.draft * a.n_heads) return;
+  const int row = (int)(id / a.n_heads), head = (int)(id - (int64_t)row * a.n_heads), d = threadIdx.x % LPR * 4;
+  const Span sp = span_of(a, row / a.draft);
+  const int n = span_plan(sp.keys, step_keys, g.smax, g.least).n;
+  if (n == 1) return;
+  const size_t base = rec_index(a, row, head, 0, g.smax);
+  float m = -INFINITY;
+  for (int s = 0; s < n; ++s) m = fmaxf(m, g.stat[base + s].x);
+  const float ref = m == -INFINITY ? 0.f : m;
+  pf_f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < n; ++s) {
+    const float2 st = g.stat[base + s];
+    const float f = __builtin_amdgcn_exp2f(st.x - ref);
+    const pf_f32x4 x = *(const pf_f32x4 *)(g.rec + (base + s) * HD + d);
+    l = fmaf(f, st.y, l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = fmaf(f, x[i], o[i]);
+  }
+  finish<T>(a, g.whole, row, head, d, o, m, l);
+}
+
+// The weights of a row's keys, from its scores and sums, added to its totals.
+__global__ __launch_bounds__(256) void span_weigh_kernel(SpanArgs a, SpanGrid g, int step_keys, int chunk, int parts) {
+  __shared__ float2 norm[64];             // of a query head: reference, 1 / sum
+  const int kv = a.map.n_kv_heads, G = a.n_heads / kv;
+  const int id = blockIdx.x / parts, head = id % kv, b = id / kv, first = (blockIdx.x - id * parts) * chunk;
+  const Span sp = span_of(a, b);
+  if (first >= sp.len) return;
+  const int n = span_plan(sp.keys, step_keys, g.smax, g.least).n;
+  for (int h = threadIdx.x; h < G; h += 256) {
+    const size_t base = rec_index(a, b, head * G + h, 0, g.smax);
+    float m = -INFINITY, l = 0.f;
+    for (int s = 0; s < n; ++s) m = fmaxf(m, g.stat[base + s].x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    for (int s = 0; s < n; ++s) l = fmaf(__builtin_amdgcn_exp2f(g.stat[base + s].x - ref), g.stat[base + s].y, l);
+    norm[h] = make_float2(ref, inverse(l));
+  }
+  __syncthreads();
+  const size_t row = (size_t)b * kv + head;
+  const float *in = a.weight + row * a.weight_ld;
+  float *out = a.weight_out + row * a.weight_out_ld;
+  const float *score = g.score + ((size_t)b * a.n_heads + head * G) * g.score_ld;
+  for (int j = first + threadIdx.x; j < min(first + chunk, sp.len); j += 256) {
+    float sum = 0.f;
+    if (page_row(a.map, sp.seq, j, head) != kNoRow) {
+      for (int h = 0; h < G; ++h) sum += __builtin_amdgcn_exp2f(score[(size_t)h * g.score_ld + j] - norm[h].x) * norm[h].y;
+    }
+    out[j] = in[j] + sum;
+  }
+}
+
+// How many splits, at most: by the workgroups that the call has without any.
+int most_splits(int64_t workgroups) { return (int)std::min<int64_t>(64, std::max<int64_t>(1, 1024 / workgroups)); }
+
+struct SpanSizes {
+  int blocks, smax, least, step;
+  size_t records, stats, scores;          // bytes
+  int64_t score_ld;
+};
+template <typename T, int HD, int NB, int WC>
+SpanSizes sizes_of(int n, int draft, int n_heads, int n_kv_heads, int keys, bool trees, bool weigh) {
+  using S = Shape<T, HD, NB, WC>;
+  SpanSizes z;
+  const int cols = draft * (n_heads / n_kv_heads);
+  z.blocks = (cols + S::COLS - 1) / S::COLS;
+  z.step = S::STEP;
+  z.least = std::max(1, 256 / S::STEP);
+  const int64_t most = (int64_t)keys + (trees ? draft : 0);
+  z.smax = most_splits((int64_t)std::max(n, 1) * n_kv_heads * z.blocks);
+  z.smax = (int)std::min<int64_t>(z.smax, std::max<int64_t>(1, (most + z.step * z.least - 1) / (z.step * z.least)));
+  const size_t heads = (size_t)n * draft * n_heads;
+  z.records = z.smax > 1 ? heads * z.smax * HD * sizeof(float) : 0;
+  z.stats = z.smax > 1 || weigh ? heads * z.smax * sizeof(float2) : 0;
+  z.stats = (z.stats + 15) / 16 * 16;
+  z.score_ld = weigh ? (most + S::STEP - 1) / S::STEP * S::STEP : 0;
+  z.scores = weigh ? (size_t)n * n_heads * z.score_ld * sizeof(float) : 0;
+  return z;
+}
+
+template <typename T, int HD, int NB, int WC>
+hipError_t go(const SpanArgs &a, hipStream_t s) {
+  using S = Shape<T, HD, NB, WC>;
+  const bool weigh = a.weight_out != nullptr;
+  const SpanSizes z = sizes_of<T, HD, NB, WC>(a.n, a.draft, a.n_heads, a.map.n_kv_heads, a.most, a.mask != nullptr, weigh);
+  SpanGrid g{};
+  g.blocks = z.blocks;
+  g.smax = z.smax;
+  g.least = z.least;
+  g.rec = (float *)a.work;
+  g.stat = (float2 *)((char *)a.work + z.records);
+  g.score = weigh ? (float *)((char *)a.work + z.records + z.stats) : nullptr;
+  g.score_ld = z.score_ld;
+  auto whole = [](const void *p, int64_t row, int64_t head) {
+    return (uintptr_t)p % 16 == 0 && row * sizeof(T) % 16 == 0 && head * sizeof(T) % 16 == 0;
+  };
+  g.whole = whole(a.q, a.q_row, a.q_head) && whole(a.out, a.out_row, a.out_head);
+  const int64_t grid = (int64_t)a.n * a.map.n_kv_heads * z.blocks * z.smax;
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  span_attn_kernel<T, HD, NB, WC><<<(unsigned)grid, 64 * S::NW, 0, s>>>(a, g);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (z.smax > 1) {
+    constexpr int PER = 256 / (HD / 4);
+    const int64_t heads = (int64_t)a.n * a.draft * a.n_heads;
+    span_join_kernel<T, HD><<<(unsigned)((heads + PER - 1) / PER), 256, 0, s>>>(a, g, z.step);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (weigh && a.max_len > 0) {
+    const int chunk = 1024;
+    const int64_t parts = ((int64_t)a.max_len + chunk - 1) / chunk, blocks = parts * a.n * a.map.n_kv_heads;
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    span_weigh_kernel<<<(unsigned)blocks, 256, 0, s>>>(a, g, z.step, chunk, (int)parts);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+// The columns a workgroup takes: as many as the call has, so that keys are read
+// by few.
+template <typename T, int HD, typename F>
+auto by_columns(int cols, F f) {
+  if (cols <= 16) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+  if (cols <= 32) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
+  if (cols <= 64) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
+  return f(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
+}
+template <typename F>
+auto by_type(int dtype, int head_dim, F f) {
+  if (dtype == DEX_F32)
+    return head_dim == 32   ? f(float(), std::integral_constant<int, 32>())
+           : head_dim == 64 ? f(float(), std::integral_constant<int, 64>())
+                            : f(float(), std::integral_constant<int, 128>());
+  return head_dim == 32   ? f(uint16_t(), std::integral_constant<int, 32>())
+         : head_dim == 64 ? f(uint16_t(), std::integral_constant<int, 64>())
+                          : f(uint16_t(), std::integral_constant<int, 128>());
+}
+
+}  // namespace
+
+size_t span_work(int dtype, int n, int draft, int n_heads, int n_kv_heads, int head_dim, int most, bool trees, bool weigh) {
+  return by_type(dtype, head_dim, [&](auto t, auto hd) {
+    return by_columns<decltype(t), hd.value>(draft * (n_heads / n_kv_heads), [&](auto nb, auto wc) {
+      const SpanSizes z = sizes_of<decltype(t), hd.value, nb.value, wc.value>(n, draft, n_heads, n_kv_heads, most, trees, weigh);
+      return z.records + z.stats + z.scores;
+    });
+  });
+}
+
+hipError_t launch_span(int dtype, const SpanArgs &a, hipStream_t s) {
+  return by_type(dtype, a.head_dim, [&](auto t, auto hd) {
+    return by_columns<decltype(t), hd.value>(a.draft * (a.n_heads / a.map.n_kv_heads), [&](auto nb, auto wc) {
+      return go<decltype(t), hd.value, nb.value, wc.value>(a, s);
+    });
+  });
+}
+
+}  // namespace dex

@@ -1,0 +1,191 @@
+// Trees of drafted tokens: masks, the accepted path, its keys and values moved
+// behind the sequence, and pages given back.
+#include "dex.h"
+#include "dex_kernels.h"
+#include "span.h"
+
+#include <algorithm>
+
+namespace dex {
+
+namespace {
+
+// A node's parent, or -1: parents come before their children, so that no chain
+// has a cycle.
+__device__ __forceinline__ int parent_of(int p, int i) { return p >= 0 && p < i ? p : -1; }
+
+// A lane a node walks to its root: mask[i] = bits of the nodes on the way.
+__global__ __launch_bounds__(kMaxDraft) void tree_mask_kernel(TreeMaskArgs a) {
+  __shared__ int parent[kMaxDraft];
+  const int i = threadIdx.x;
+  const size_t at = (size_t)blockIdx.x * a.draft + i;
+  if (i < a.draft) parent[i] = parent_of(a.parent[at], i);
+  __syncthreads();
+  if (i >= a.draft) return;
+  uint64_t bits[kMaxDraft / 64] = {};
+  int depth = -1;
+  for (int j = i; j >= 0; j = parent[j]) {
+    ++depth;
+#pragma unroll
+    for (int w = 0; w < kMaxDraft / 64; ++w)
+      if (j >> 6 == w) bits[w] |= 1ull << (j & 63);
+  }
+#pragma unroll
+  for (int w = 0; w < kMaxDraft / 64; ++w)
+    if (w < a.words) a.mask[at * a.words + w] = bits[w];
+  if (a.depth != nullptr) a.depth[at] = depth;
+}
+
+// A lane a node walks to its root and sees whether every token on the way is
+// the one wanted; the deepest such node wins, the lowest number among equals.
+__global__ __launch_bounds__(kMaxDraft) void tree_accept_kernel(TreeAcceptArgs a) {
+  __shared__ int parent[kMaxDraft], token[kMaxDraft], target[kMaxDraft], path[kMaxDraft], best;
+  const int i = threadIdx.x, b = blockIdx.x;
+  const size_t at = (size_t)b * a.draft + i;
+  const int n = a.n_draft != nullptr ? max(0, min(a.n_draft[b], a.draft)) : a.draft;
+  if (i < n) {
+    parent[i] = parent_of(a.parent[at], i);
+    token[i] = a.token[at];
+    target[i] = a.target[at];
+  }
+  path[i] = -1;
+  if (i == 0) best = 0;
+  __syncthreads();
+  if (i < n) {
+    int depth = 0;
+    bool ok = true;
+    for (int j = i; j >= 0 && ok; j = parent[j]) {
+      ++depth;
+      const int p = parent[j];
+      ok = p >= 0 ? token[j] == target[p] : a.root == nullptr || token[j] == a.root[b];
+    }
+    if (ok) atomicMax(&best, depth << 16 | (0xffff - i));
+  }
+  __syncthreads();
+  const int depth = best >> 16, last = 0xffff - (best & 0xffff);
+  if (i == 0) {
+    int at_depth = depth;
+    if (depth > 0)
+      for (int j = last; j >= 0; j = parent[j]) path[--at_depth] = j;
+    a.count[b] = depth;
+    a.next[b] = depth > 0 ? target[last] : a.root != nullptr ? a.root[b] : -1;
+  }
+  __syncthreads();
+  if (i < a.draft) a.path[at] = path[i];
+}
+
+// Entries of a (layer, sequence, kv head), a slice of their rows' 16-byte
+// chunks.  In place the entries go in turns: a turn's loads are all done before
+// its first store, and a source is never before its own destination, so it is
+// behind all earlier ones and no store overtakes a load.
+constexpr int KEEP_THREADS = 256, KEEP_EACH = 8;
+__global__ __launch_bounds__(KEEP_THREADS) void keep_kernel(KeepArgs a, int lanes, int slices, int turns) {
+  const int kv = a.map.n_kv_heads;
+  int x = blockIdx.x;
+  const int slice = x % slices;
+  x /= slices;
+  const int head = x % kv;
+  x /= kv;
+  const int layer = x % a.n_layers, s = x / a.n_layers;
+  const int n = min(a.count[s], a.capacity);
+  const int first = a.first != nullptr ? a.first[s] : 0;
+  const int chunk = slice * lanes + threadIdx.x % lanes, per = KEEP_THREADS / lanes, j_lane = threadIdx.x / lanes;
+  if (first < 0) return;
+  const int *index = a.index + layer * a.index_layer + s * a.index_seq + head * a.index_head;
+  const bool in_place = a.to == nullptr;
+  PageMap to = a.map;
+  if (!in_place) to.table = a.to, to.max_pages = a.to_pages;
+  const size_t base = (size_t)layer * a.map.n_pages * kv << a.map.shift;     // rows before the layer's
+  const bool mine = chunk * 16 < a.row_bytes && j_lane < per;
+  const int turn = per * KEEP_EACH;
+  const int j_first = blockIdx.y * turns * turn, j_end = min(n, j_first + turns * turn);
+  for (int j0 = j_first; j0 < j_end; j0 += turn) {
+    typedef __attribute__((ext_vector_type(4))) uint32_t chunk_t;
+    chunk_t k[KEEP_EACH], v[KEEP_EACH];
+    size_t dst[KEEP_EACH];
+    bool go[KEEP_EACH];
+#pragma unroll
+    for (int e = 0; e < KEEP_EACH; ++e) {
+      const int j = j0 + e * per + j_lane;
+      go[e] = mine && j < j_end;
+      uint32_t from = kNoRow, into = kNoRow;
+      if (go[e]) {
+        const int i = index[j];
+        if (i >= 0 && i <= (1 << 30) && first <= (1 << 30) && !(in_place && i <= j)) {
+          from = page_row(a.map, s, first + i, head);
+          into = page_row(to, s, first + j, head);
+        }
+      }
+      go[e] = from != kNoRow && into != kNoRow;
+      // (one that copies nothing reads the layer's first row)
+      const size_t src = (base + (go[e] ? from : 0)) * a.row_bytes + (mine ? chunk : 0) * 16;
+      dst[e] = (base + (go[e] ? into : 0)) * a.row_bytes + chunk * 16;
+      k[e] = *(const chunk_t *)((const char *)a.k + src);
+      v[e] = *(const chunk_t *)((const char *)a.v + src);
+    }
+    if (in_place) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+    }
+#pragma unroll
+    for (int e = 0; e < KEEP_EACH; ++e)
+      if (go[e]) {
+        *(chunk_t *)((char *)a.k + dst[e]) = k[e];
+        *(chunk_t *)((char *)a.v + dst[e]) = v[e];
+      }
+  }
+}
+
+// Pages behind a sequence's last token leave its row of the table.
+__global__ __launch_bounds__(256) void trim_copy_kernel(TrimArgs a) {
+  for (int p = blockIdx.x * 256 + threadIdx.x; p < a.n_pages; p += gridDim.x * 256) a.ref_out[p] = a.ref[p];
+}
+__global__ __launch_bounds__(256) void trim_kernel(TrimArgs a) {
+  const int64_t entries = (int64_t)a.n_seqs * a.max_pages;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < entries; e += (int64_t)gridDim.x * 256) {
+    const int s = (int)(e / a.max_pages), c = (int)(e - (int64_t)s * a.max_pages);
+    int p = a.table[e];
+    if ((int64_t)c << a.shift >= max(0, a.len[s])) {
+      if (p >= 0 && p < a.n_pages) atomicSub(&a.ref_out[p], 1);
+      p = -1;
+    }
+    a.table_out[e] = p;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_tree_mask(const TreeMaskArgs &a, hipStream_t s) {
+  tree_mask_kernel<<<a.n, (a.draft + 63) / 64 * 64, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_tree_accept(const TreeAcceptArgs &a, hipStream_t s) {
+  tree_accept_kernel<<<a.n, kMaxDraft, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_keep(const KeepArgs &a, hipStream_t s) {
+  const int chunks = a.row_bytes / 16;
+  const int lanes = std::min(chunks, 8), slices = (chunks + lanes - 1) / lanes;
+  const int turn = KEEP_THREADS / lanes * KEEP_EACH, all = (a.capacity + turn - 1) / turn;
+  const int64_t blocks = (int64_t)a.map.n_seqs * a.n_layers * a.map.n_kv_heads * slices;
+  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  const int split = a.to == nullptr ? 1 : std::min(all, 65535), turns = (all + split - 1) / split;
+  keep_kernel<<<dim3((unsigned)blocks, split), KEEP_THREADS, 0, s>>>(a, lanes, slices, turns);
+  return hipGetLastError();
+}
+
+hipError_t launch_trim(const TrimArgs &a, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (a.ref_out != a.ref) {
+    trim_copy_kernel<<<std::min((a.n_pages + 255) / 256, 1024), 256, 0, s>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const int64_t entries = (int64_t)a.n_seqs * a.max_pages;
+  trim_kernel<<<(unsigned)std::min<int64_t>((entries + 255) / 256, 2048), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace dex

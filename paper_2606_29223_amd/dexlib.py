@@ -31,6 +31,9 @@ EXPORTED = (
     "dex_rotary_turns", "dex_rope", "dex_pages_append", "dex_pages_attention", "dex_pages_attention_work",
     "dex_pages_fork", "dex_pages_reserve", "dex_pages_compact", "dex_pages_copy", "dex_beam_select",
     "dex_beam_select_work",
+    "dex_tree_mask", "dex_tree_accept", "dex_pages_tree_attention", "dex_pages_tree_attention_work", "dex_pages_keep",
+    "dex_pages_trim", "dex_pages_bounds", "dex_pages_select", "dex_pages_select_work", "dex_pages_sparse_attention",
+    "dex_pages_sparse_attention_work", "dex_pages_weigh", "dex_pages_weigh_work", "dex_pages_evict",
 )
 
 
@@ -133,6 +136,26 @@ def load(path: str | None = None):
     lib.dex_pages_copy.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp]
     lib.dex_beam_select_work.argtypes = [i32] * 5
     lib.dex_beam_select.argtypes = [i32, vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
+    pages = [vp, vp, i32, i32, vp, i32, i32]         # keys, values, n_pages, page_size, table, n_seqs, max_pages
+    lib.dex_tree_mask.argtypes = [vp, i32, i32, vp, vp, vp]
+    lib.dex_tree_accept.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+    lib.dex_pages_tree_attention_work.argtypes = [i32] * 7
+    lib.dex_pages_tree_attention.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, i32, f32, *heads, vp, *pages,
+                                             *heads, vp, vp, vp]
+    lib.dex_pages_keep.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, i32, i32, vp, i32, vp, vp, i64, i64, i64,
+                                   i32, vp, vp]
+    lib.dex_pages_trim.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
+    lib.dex_pages_bounds.argtypes = [i32, i32, vp, i32, i32, i32, vp, i32, i32, vp, i32, vp, vp]
+    lib.dex_pages_select_work.argtypes = [i32] * 4
+    lib.dex_pages_select.argtypes = [i32, i32, i32, i32, i32, vp, vp, i32, *heads, vp, i32, i32, vp, i32, i32, i32,
+                                     i32, i32, vp, vp, vp]
+    lib.dex_pages_sparse_attention_work.argtypes = [i32] * 7
+    lib.dex_pages_sparse_attention.argtypes = [i32, i32, i32, i32, i32, vp, vp, f32, *heads, vp, i32, *pages, *heads,
+                                               vp, vp, vp]
+    lib.dex_pages_weigh_work.argtypes = [i32] * 6
+    lib.dex_pages_weigh.argtypes = [i32, i32, i32, i32, i32, vp, vp, i32, f32, *heads, vp, i64, vp, i64, *pages, *heads,
+                                    vp, vp, vp]
+    lib.dex_pages_evict.argtypes = [vp, i64, i32, i32, i32, vp, i32, i32, i32, vp, vp, vp, i64, vp]
     for name in EXPORTED:
         if name.endswith("_work"):
             getattr(lib, name).restype = i64

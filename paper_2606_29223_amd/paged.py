@@ -1,6 +1,7 @@
 """Operators over a paged key/value cache on torch tensors (include/dex.h,
 same names): rotary positions and the cache write, attention of one new token
-a row, page tables that fork, grow and compact, and beam selection.
+a row, page tables that fork, grow and compact, beam selection; trees of drafted
+tokens, attention over chosen pages, and eviction by accumulated weight.
 
 A cache is plain tensors of the caller: a layer's keys and values are
 [n_pages, n_kv_heads, page_size, head_dim] each, a pool of layers
@@ -25,6 +26,20 @@ A step of a decoding loop with branches, for a model of the caller's:
         out = cache.attention(layer, q, group=beams)
     parent, token, score, done = paged.beam_select(logits, score, done=done, eos=eos)
     cache.fork(parent.flatten())                      # the branches follow their parents
+
+A step with drafted tokens, `draft` of them a sequence in trees:
+
+    mask, depth = paged.tree_mask(parent)
+    before = cache.lens.clone()
+    pos = cache.reserve(n_draft).pos                   # n_draft: draft for every sequence
+    at = (before[:, None] + depth).flatten()           # rotary positions
+    place = (pos[:, None] + torch.arange(draft, dtype=torch.int32, device=pos.device)).flatten()
+    for layer in range(cache.n_layers):
+        q, k = paged.rope(rotary, at, q, k)
+        cache.append(layer, place, q, k, v, seq=seq)   # seq: each row's sequence
+        out = cache.tree_attention(layer, q, before, mask)
+    path, count, token = paged.tree_accept(parent, drafted, target)
+    cache.accept(before, path, count)                  # the path's tokens stay, the others go
 """
 
 from __future__ import annotations
@@ -405,18 +420,336 @@ def beam_select(logits, scores, n_out=None, done=None, eos=-1):
     return parent, token, score, ends
 
 
+# ------------------------------------------ trees, chosen pages and eviction
+
+_MAX_DRAFT = 256
+
+
+@functools.lru_cache(maxsize=4096)
+def _tree_work(*sizes):
+    return dexlib.load().dex_pages_tree_attention_work(*sizes)
+
+
+@functools.lru_cache(maxsize=4096)
+def _sparse_work(*sizes):
+    return dexlib.load().dex_pages_sparse_attention_work(*sizes)
+
+
+@functools.lru_cache(maxsize=4096)
+def _weigh_work(*sizes):
+    return max(16, dexlib.load().dex_pages_weigh_work(*sizes))
+
+
+def _bytes(n, device):
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _trees(parent):
+    """Checks [n, draft] int32 on a GPU: device, n, draft."""
+    if parent.device.type != "cuda":
+        _refuse("parent is not on a GPU")
+    if parent.dim() != 2 or not 1 <= parent.shape[1] <= _MAX_DRAFT:
+        _refuse(f"parent is [n_trees, draft], draft 1 to {_MAX_DRAFT}")
+    return parent.device, parent.shape[0], parent.shape[1]
+
+
+def tree_mask(parent):
+    """Trees of drafted tokens, parent [n, draft] int32: node i continues node
+    parent[i] < i, or is a root (-1).  Returns mask [n, draft, words] int64, bit j
+    of row i set if j is node i or an ancestor, and depth [n, draft] int32."""
+    dev, n, t = _trees(parent)
+    p = _ints(parent, dev, (n, t), "parent")
+    mask = torch.empty((n, t, (t + 63) // 64), dtype=torch.int64, device=dev)
+    depth = torch.empty_like(parent)
+    if n > 0:
+        _run(dexlib.load().dex_tree_mask, dev, p, n, t, mask.data_ptr(), depth.data_ptr())
+    return mask, depth
+
+
+def tree_accept(parent, token, target, n_draft=None, root=None):
+    """The path of each tree that the model agrees with: node i is accepted if its
+    parent is and token[i] == target[parent[i]] (all [n, draft] int32), a root if
+    token[i] == root (root [n] int32; always without it); nodes from n_draft [n]
+    on are none.  Returns path [n, draft] (nodes from a root to the deepest
+    accepted one, then -1), count [n] and the next token [n]."""
+    dev, n, t = _trees(parent)
+    shape = (n, t)
+    args = [_ints(x, dev, shape, name) for x, name in ((parent, "parent"), (token, "token"), (target, "target"))]
+    nd = None if n_draft is None else _ints(n_draft, dev, (n,), "n_draft")
+    r = None if root is None else _ints(root, dev, (n,), "root")
+    path = torch.empty_like(parent)
+    both = torch.empty((2, n), dtype=torch.int32, device=dev)
+    if n > 0:
+        at = both.data_ptr()
+        _run(dexlib.load().dex_tree_accept, dev, *args, nd, r, n, t, path.data_ptr(), at, at + 4 * n)
+    return path, both[0], both[1]
+
+
+def _max_len(max_len, most):
+    if max_len is None or max_len > most:
+        return most
+    if max_len < 0:
+        _refuse("max_len is below 0")
+    return max_len
+
+
+def tree_attention(q, k_pages, v_pages, table, lens, mask, n_draft=None, seq=None, max_len=None, scale=None, out=None,
+                   return_lse=False):
+    """Attention of drafted tokens: q [n * draft, heads, head_dim], `draft` rows
+    a tree, over the first lens[b] keys of sequence seq[b] (b without `seq`) and
+    the drafted keys at positions lens[b] + j whose bit is set in mask[b, i]
+    (`tree_mask`; any other mask works), j < n_draft[b].  `max_len` bounds lens.
+    Returns out, or (out, lse); a row that sees nothing, and the rows from
+    n_draft[b] on, get 0 and -inf."""
+    _detached(q, k_pages, v_pages, out)
+    d, (n_pages, kv, ps, hd) = _pages(k_pages, v_pages, table)
+    dev, dt = k_pages.device, k_pages.dtype
+    if q.dim() != 3:
+        _refuse("queries are [n_trees * draft, heads, head_dim]")
+    if mask.dim() != 3 or mask.dtype is not torch.int64 or mask.device != dev or not mask.is_contiguous():
+        _refuse("mask is a contiguous int64 [n_trees, draft, words] tensor on the cache's device")
+    n, t, words = mask.shape
+    if not 1 <= t <= _MAX_DRAFT or words != (t + 63) // 64:
+        _refuse(f"mask has 1 to {_MAX_DRAFT} drafted rows of ceil(draft / 64) words")
+    heads = q.shape[1]
+    shape = (n * t, heads, hd)
+    a = _heads(q, dev, dt, shape, "q")
+    out, o = _out(out, q, shape, "out")
+    ts = table.shape
+    tab = _ints(table, dev, ts, "table")
+    length = _ints(lens, dev, (n,), "lens")
+    nd = None if n_draft is None else _ints(n_draft, dev, (n,), "n_draft")
+    s = None if seq is None else _ints(seq, dev, (n,), "seq")
+    max_len = _max_len(max_len, ts[1] * ps)
+    lse = torch.empty((n * t, heads), dtype=torch.float32, device=dev) if return_lse else None
+    if n > 0:
+        work = _bytes(_tree_work(d, n, t, heads, kv, hd, max_len), dev)
+        _run(dexlib.load().dex_pages_tree_attention, dev, d, hd, heads, kv, n, t, s, length, nd, max_len,
+             1.0 / math.sqrt(hd) if scale is None else scale, *a, mask.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+             n_pages, ps, tab, ts[0], ts[1], *o, None if lse is None else lse.data_ptr(),
+             None if work is None else work.data_ptr())
+    return (out, lse) if return_lse else out
+
+
+def keep(k_pool, v_pool, table, index, count, first=None, to=None):
+    """Position first[s] + j of sequence s receives keys and values of its
+    position first[s] + index[j], j < count[s], in every layer of the pools
+    [n_layers, n_pages, n_kv_heads, page_size, head_dim]; count and first (0
+    without it) are [n_seqs] int32.  index is [n_seqs, n], the same for all, or
+    [n_seqs, n_kv_heads, n], or [n_layers, n_seqs, n_kv_heads, n].  In place an
+    entry with index[j] <= j copies nothing; `to` [n_seqs, pages] is another
+    table to write to.  Pages written to have no other holder."""
+    _detached(k_pool, v_pool)
+    d = _gpu(k_pool, "k_pool")
+    dev = k_pool.device
+    if k_pool.dim() != 5 or not k_pool.is_contiguous():
+        _refuse("pools are contiguous [n_layers, n_pages, n_kv_heads, page_size, head_dim]")
+    if (v_pool.dtype is not k_pool.dtype or v_pool.device != dev or v_pool.shape != k_pool.shape
+            or not v_pool.is_contiguous()):
+        _refuse("values and keys differ in type, device or shape")
+    layers, n_pages, kv, ps, hd = k_pool.shape
+    if table.dim() != 2 or (to is not None and to.dim() != 2):
+        _refuse("tables are [n_seqs, max_pages]")
+    n = table.shape[0]
+    lists = {2: (n,), 3: (n, kv), 4: (layers, n, kv)}.get(index.dim())
+    if lists is None or tuple(index.shape[:-1]) != lists:
+        _refuse("index is [n_seqs, n], [n_seqs, n_kv_heads, n] or [n_layers, n_seqs, n_kv_heads, n]")
+    cap = index.shape[-1]
+    at = _ints(index, dev, index.shape, "index")
+    many = kv if index.dim() > 2 else 1
+    strides = (n * many * cap if index.dim() == 4 else 0, many * cap, cap if many > 1 else 0)
+    c = _ints(count, dev, (n,), "count")
+    f = None if first is None else _ints(first, dev, (n,), "first")
+    tab = _ints(table, dev, table.shape, "table")
+    other, width = (None, 0) if to is None else (_ints(to, dev, (n, to.shape[1]), "to"), to.shape[1])
+    if n > 0 and cap > 0:
+        _run(dexlib.load().dex_pages_keep, dev, d, hd, layers, n_pages, kv, ps, k_pool.data_ptr(), v_pool.data_ptr(), tab, n,
+             table.shape[1], other, width, f, at, *strides, cap, c)
+
+
+def trim(table, ref, lens, page_size, out=None):
+    """Pages behind the sequences' last tokens (lens) leave the table and lose a
+    holder.  out: (table, ref) to write to; without it both change in place.
+    Returns them."""
+    dev, p = _tables(table, ref, lens)
+    if not 1 <= page_size <= 1024:
+        _refuse("page_size is not a power of two up to 1024")
+    t, r = (table, ref) if out is None else out
+    _run(dexlib.load().dex_pages_trim, dev, *p, table.shape[0], table.shape[1], ref.shape[0], page_size,
+         _ints(t, dev, table.shape, "out[0]"), _ints(r, dev, ref.shape, "out[1]"))
+    return t, r
+
+
+def _bounds(bounds, k_dtype, dev, shape, name="bounds"):
+    if bounds.dtype is not k_dtype or bounds.device != dev or bounds.shape != shape or not bounds.is_contiguous():
+        _refuse(f"{name}: a contiguous {k_dtype} tensor of shape {tuple(shape)} on {dev} is wanted")
+    return bounds.data_ptr()
+
+
+def page_bounds(k_pages, table, lens, n_new=None, out=None):
+    """The least and the largest key of each page in every dimension, [n_pages,
+    n_kv_heads, 2, head_dim]: those of the pages that hold the last n_new (all
+    without it) of lens[s] tokens of the sequences, in `out` (0 elsewhere in a
+    new one)."""
+    _detached(k_pages, out)
+    d, (n_pages, kv, ps, hd) = _pages(k_pages, k_pages, table)
+    dev = k_pages.device
+    shape = (n_pages, kv, 2, hd)
+    out = k_pages.new_zeros(shape) if out is None else out
+    at = _bounds(out, k_pages.dtype, dev, shape, "out")
+    ts = table.shape
+    tab, length = _ints(table, dev, ts, "table"), _ints(lens, dev, (ts[0],), "lens")
+    n_new = _max_len(n_new, ts[1] * ps)
+    if ts[0] > 0:
+        _run(dexlib.load().dex_pages_bounds, dev, d, hd, k_pages.data_ptr(), n_pages, kv, ps, tab, ts[0], ts[1], length, n_new,
+             at)
+    return out
+
+
+def select_pages(q, bounds, table, lens, page_size, n_select, sinks=1, recent=1, seq=None, max_len=None):
+    """The pages to read for each row and kv head: q [rows, heads, head_dim],
+    bounds as `page_bounds` gives them.  Of the table's columns that hold tokens,
+    the first `sinks`, the last `recent` and those whose bounds allow the largest
+    products with the kv head's queries, n_select in all.  Returns columns [rows,
+    n_kv_heads, n_select] int32, ascending, then -1."""
+    _detached(q, bounds)
+    d = _gpu(bounds, "bounds")
+    dev, dt = bounds.device, bounds.dtype
+    if bounds.dim() != 4 or bounds.shape[2] != 2 or not bounds.is_contiguous():
+        _refuse("bounds are contiguous [n_pages, n_kv_heads, 2, head_dim]")
+    n_pages, kv, _, hd = bounds.shape
+    if q.dim() != 3 or table.dim() != 2:
+        _refuse("queries are [rows, heads, head_dim], table is [n_seqs, max_pages]")
+    rows, heads = q.shape[:2]
+    a = _heads(q, dev, dt, (rows, heads, hd), "q")
+    ts = table.shape
+    tab, length = _ints(table, dev, ts, "table"), _ints(lens, dev, (rows,), "lens")
+    s = None if seq is None else _ints(seq, dev, (rows,), "seq")
+    if not 1 <= page_size <= 1024:
+        _refuse("page_size is not a power of two up to 1024")
+    max_len = _max_len(max_len, ts[1] * page_size)
+    if not 1 <= n_select < 1 << 31 or not 0 <= sinks <= n_select or not 0 <= recent <= n_select:
+        _refuse("n_select is below 1 or below sinks + recent")
+    columns = torch.empty((rows, kv, n_select), dtype=torch.int32, device=dev)
+    if rows > 0:
+        work = torch.empty(rows * kv * -(-max_len // page_size), dtype=torch.int64, device=dev)
+        _run(dexlib.load().dex_pages_select, dev, d, hd, heads, kv, rows, s, length, max_len, *a, bounds.data_ptr(), n_pages,
+             page_size, tab, ts[0], ts[1], n_select, sinks, recent, columns.data_ptr(), work.data_ptr())
+    return columns
+
+
+def sparse_attention(q, k_pages, v_pages, table, lens, columns, seq=None, scale=None, out=None, return_lse=False):
+    """`attention` over the tokens of the listed columns of the table alone,
+    columns [rows, n_kv_heads, n] int32 as `select_pages` gives them."""
+    _detached(q, k_pages, v_pages, out)
+    d, (n_pages, kv, ps, hd) = _pages(k_pages, v_pages, table)
+    dev, dt = k_pages.device, k_pages.dtype
+    if q.dim() != 3 or columns.dim() != 3:
+        _refuse("queries are [rows, heads, head_dim], columns [rows, n_kv_heads, n]")
+    rows, heads = q.shape[:2]
+    shape = (rows, heads, hd)
+    a = _heads(q, dev, dt, shape, "q")
+    out, o = _out(out, q, shape, "out")
+    ts, n = table.shape, columns.shape[2]
+    tab, length = _ints(table, dev, ts, "table"), _ints(lens, dev, (rows,), "lens")
+    c = _ints(columns, dev, (rows, kv, n), "columns")
+    s = None if seq is None else _ints(seq, dev, (rows,), "seq")
+    lse = torch.empty((rows, heads), dtype=torch.float32, device=dev) if return_lse else None
+    if rows > 0:
+        work = _bytes(_sparse_work(d, rows, heads, kv, hd, n, ps), dev)
+        _run(dexlib.load().dex_pages_sparse_attention, dev, d, hd, heads, kv, rows, s, length,
+             1.0 / math.sqrt(hd) if scale is None else scale, *a, c, n, k_pages.data_ptr(), v_pages.data_ptr(), n_pages, ps,
+             tab, ts[0], ts[1], *o, None if lse is None else lse.data_ptr(), None if work is None else work.data_ptr())
+    return (out, lse) if return_lse else out
+
+
+def _weights(t, dev, rows, kv, name):
+    """[rows, n_kv_heads, n] float32, contiguous: its address."""
+    if (t.dtype is not torch.float32 or t.device != dev or t.dim() != 3 or t.shape[:2] != (rows, kv)
+            or not t.is_contiguous()):
+        _refuse(f"{name} is a contiguous float32 [{rows}, {kv}, n] tensor on {dev}")
+    return t.data_ptr()
+
+
+def weigh(q, k_pages, v_pages, table, lens, weight, weight_out=None, seq=None, max_len=None, scale=None, out=None,
+          return_lse=False):
+    """`attention` of one new token a row that also adds up what each key was
+    given: weight_out[r, h, j] = weight[r, h, j] + the softmax weights of key j <
+    lens[r], summed over the query heads of kv head h; float32 [rows, n_kv_heads,
+    n], n at least max_len.  Without weight_out in place; what lies behind
+    lens[r] stays.  Returns out, or (out, lse)."""
+    _detached(q, k_pages, v_pages, weight, weight_out, out)
+    d, (n_pages, kv, ps, hd) = _pages(k_pages, v_pages, table)
+    dev, dt = k_pages.device, k_pages.dtype
+    if q.dim() != 3:
+        _refuse("queries are [rows, heads, head_dim]")
+    rows, heads = q.shape[:2]
+    shape = (rows, heads, hd)
+    a = _heads(q, dev, dt, shape, "q")
+    out, o = _out(out, q, shape, "out")
+    ts = table.shape
+    tab, length = _ints(table, dev, ts, "table"), _ints(lens, dev, (rows,), "lens")
+    s = None if seq is None else _ints(seq, dev, (rows,), "seq")
+    max_len = _max_len(max_len, ts[1] * ps)
+    w = _weights(weight, dev, rows, kv, "weight")
+    to, wo = (weight, w) if weight_out is None else (weight_out, _weights(weight_out, dev, rows, kv, "weight_out"))
+    if min(weight.shape[2], to.shape[2]) < max_len:
+        _refuse("the weights have fewer columns than max_len")
+    lse = torch.empty((rows, heads), dtype=torch.float32, device=dev) if return_lse else None
+    if rows > 0:
+        work = _bytes(_weigh_work(d, rows, heads, kv, hd, max_len), dev)
+        _run(dexlib.load().dex_pages_weigh, dev, d, hd, heads, kv, rows, s, length, max_len,
+             1.0 / math.sqrt(hd) if scale is None else scale, *a, w, weight.shape[2], wo, to.shape[2], k_pages.data_ptr(),
+             v_pages.data_ptr(), n_pages, ps, tab, ts[0], ts[1], *o, None if lse is None else lse.data_ptr(), work.data_ptr())
+    return (out, lse) if return_lse else out
+
+
+def evict(weight, lens, budget, sinks=0, recent=1, weight_out=None):
+    """Which keys of each sequence and kv head stay, by their accumulated weight
+    [n_seqs, n_kv_heads, n] float32: the first `sinks`, the last `recent` and the
+    heaviest others, min(lens[s], budget) in all.  Returns index [n_seqs,
+    n_kv_heads, budget] int32, ascending, then -1, as `keep` takes it, and count
+    [n_seqs], the sequences' new lengths; weight_out (`weight` without it)
+    receives the kept keys' weights, then 0."""
+    _detached(weight, weight_out)
+    if weight.device.type != "cuda":
+        _refuse("weight is not on a GPU")
+    dev = weight.device
+    if weight.dim() != 3:
+        _refuse("weight is [n_seqs, n_kv_heads, n]")
+    n, kv, cap = weight.shape
+    w = _weights(weight, dev, n, kv, "weight")
+    to = weight if weight_out is None else weight_out
+    wo = _weights(to, dev, n, kv, "weight_out")
+    if to.shape != weight.shape:
+        _refuse("weight_out has another shape than weight")
+    length = _ints(lens, dev, (n,), "lens")
+    if not 1 <= budget < 1 << 31 or not 0 <= sinks <= budget or not 0 <= recent <= budget:
+        _refuse("budget is below 1 or below sinks + recent")
+    index = torch.empty((n, kv, budget), dtype=torch.int32, device=dev)
+    count = torch.empty(n, dtype=torch.int32, device=dev)
+    if n > 0:
+        _run(dexlib.load().dex_pages_evict, dev, w, cap, n, kv, cap, length, budget, sinks, recent, index.data_ptr(),
+             count.data_ptr(), wo, cap)
+    return index, count
+
+
+
 class PagedCache:
     """Keys and values of every layer in pages, with the page table, the
-    holders' counts and the lengths of n_seqs sequences, all free at first."""
+    holders' counts and the lengths of n_seqs sequences, all free at first; with
+    `bounds` each layer's page bounds too."""
 
     def __init__(self, n_layers, n_kv_heads, head_dim, page_size, n_pages, n_seqs, max_pages, dtype=torch.bfloat16,
-                 device="cuda"):
+                 device="cuda", bounds=False):
         shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
         self.k = torch.zeros(shape, dtype=dtype, device=device)
         self.v = torch.zeros(shape, dtype=dtype, device=device)
         self.table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device)
         self.ref = torch.zeros(n_pages, dtype=torch.int32, device=device)
         self.lens = torch.zeros(n_seqs, dtype=torch.int32, device=device)
+        # with `bounds`: each layer's, for attention over chosen pages
+        self.bounds = torch.zeros((n_layers, n_pages, n_kv_heads, 2, head_dim), dtype=dtype, device=device) if bounds else None
         self.n_layers, self.page_size = n_layers, page_size
         self._copies = False                      # whether `copy` is known to take these pools
 
@@ -454,3 +787,49 @@ class PagedCache:
         got = compact(self.table, self.ref)
         copy(self.k, self.v, got.src, got.dst, got.state)
         return got
+
+    def tree_attention(self, layer, q, lens, mask, **kw):
+        """Attention of drafted tokens over a layer; lens: the sequences' tokens
+        before their trees."""
+        return tree_attention(q, self.k[layer], self.v[layer], self.table, lens, mask, **kw)
+
+    def accept(self, lens, path, count):
+        """Of the tokens from lens [n_seqs] on, those of the path (`tree_accept`)
+        stay, behind the sequence; the rest and their pages are given back."""
+        keep(self.k, self.v, self.table, path, count, first=lens)
+        torch.add(lens, count, out=self.lens)
+        trim(self.table, self.ref, self.lens, self.page_size)
+
+    def update_bounds(self, layer, n_new=None):
+        """The bounds of the pages that hold the last n_new tokens (all without
+        it); after `fork`, `reserve` and `append` those of the new tokens, after
+        `compact` or `evict` all."""
+        if self.bounds is None:
+            _refuse("the cache keeps no bounds (bounds=True)")
+        page_bounds(self.k[layer], self.table, self.lens, n_new=n_new, out=self.bounds[layer])
+
+    def sparse_attention(self, layer, q, n_select, sinks=1, recent=1, **kw):
+        """Attention of row r over the n_select pages of sequence r that its query
+        selects (`update_bounds` has to have seen its tokens)."""
+        if self.bounds is None:
+            _refuse("the cache keeps no bounds (bounds=True)")
+        columns = select_pages(q, self.bounds[layer], self.table, self.lens, self.page_size, n_select, sinks=sinks, recent=recent)
+        return sparse_attention(q, self.k[layer], self.v[layer], self.table, self.lens, columns, **kw)
+
+    def weigh(self, layer, q, weight, **kw):
+        """Attention of row r over sequence r that adds its weights to `weight`."""
+        return weigh(q, self.k[layer], self.v[layer], self.table, self.lens, weight, **kw)
+
+    def evict(self, weight, budget, sinks=0, recent=1):
+        """Cuts every sequence to its `budget` heaviest keys (see `evict`), in place,
+        by weight [n_layers, n_seqs, n_kv_heads, n], which is cut with it.  The
+        sequences' pages have no other holders.  The keys keep the rotary positions
+        that they have, and new tokens need positions of the caller's own count."""
+        if weight.dim() != 4 or weight.shape[:3] != (self.n_layers, len(self.lens), self.k.shape[2]):
+            _refuse("weight is [n_layers, n_seqs, n_kv_heads, n]")
+        self._check_copy()
+        n = len(self.lens)
+        index, count = evict(weight.flatten(0, 1), self.lens.repeat(self.n_layers), budget, sinks=sinks, recent=recent)
+        keep(self.k, self.v, self.table, index.unflatten(0, (self.n_layers, n)), count[:n])
+        self.lens.copy_(count[:n])
+        trim(self.table, self.ref, self.lens, self.page_size)
