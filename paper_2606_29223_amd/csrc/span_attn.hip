@@ -10,6 +10,7 @@
 #include "span.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace dex {
 
@@ -26,9 +27,9 @@ struct SpanPlan {
   int steps, n;
 };
 __host__ __device__ __forceinline__ SpanPlan span_plan(int keys, int step_keys, int smax, int least) {
-  const int all = (keys + step_keys - 1) / step_keys;
+  const int all = (keys + step_keys - 1) / step_keys, n = max(1, min(smax, all / least));
   SpanPlan p;
-  p.steps = max(least, (all + smax - 1) / smax);
+  p.steps = max(1, (all + n - 1) / n);
   p.n = max(1, (all + p.steps - 1) / p.steps);
   return p;
 }
@@ -80,17 +81,20 @@ __device__ __forceinline__ float quarters_sum(float v) {
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
-__device__ __forceinline__ float after_upper(float a) {
-  return fmaxf(a - __uint_as_float(__float_as_uint(a) & 0xffff0000u), 0x1p-100f);
+__device__ __forceinline__ float after_upper(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xffff0000u); }
+// (positive bf16 compare as integers: one instruction for two)
+__device__ __forceinline__ uint32_t some_halves(uint32_t x) {
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), (u16x2)(uint16_t)0x0d80));
 }
 
 // A tile of keys or values in LDS: TK rows of HD elements, whose 16-byte chunks
 // are swapped within a row (chunk c lies at c ^ swizzle) so that the 16 rows of
 // a key fragment, and the rows that half a wave reads of the values, lie in
 // different banks.  Filled by direct transfers of 1 KB, RPT rows each.
-template <typename T, int HD>
+template <typename T, int HD, int KEYS>
 struct Tile {
-  static constexpr int TK = sizeof(T) == 2 ? 32 : 16;
+  static constexpr int TK = KEYS;
   static constexpr int NT = TK / 16, DT = HD / 16;
   static constexpr int RB = HD * sizeof(T), CPR = RB / 16, RPT = 64 / CPR, NTR = TK / RPT;
   static constexpr int BYTES = TK * RB;
@@ -105,13 +109,12 @@ struct Tile {
 
 // One wave's columns: 16 NB of them, column r16 of block nb; its scores and
 // outputs of them on the matrix cores.
-template <typename T, int HD, int NB>
+template <typename L, typename T, int HD, int NB>
 struct Cols;
 
-template <int HD, int NB>
-struct Cols<uint16_t, HD, NB> {
-  using L = Tile<uint16_t, HD>;
-  static constexpr int KS = HD / 32, NT = L::NT, DT = L::DT, CPR = L::CPR;
+template <typename L, int HD, int NB>
+struct Cols<L, uint16_t, HD, NB> {
+  static constexpr int KS = HD / 32, NT = L::NT, ST = NT / 2, DT = L::DT, CPR = L::CPR;
   pf_bf16x8 q[NB][KS];
   pf_f32x4 o[NB][DT];
 
@@ -134,75 +137,143 @@ struct Cols<uint16_t, HD, NB> {
       q[nb][st] = __builtin_bit_cast(pf_bf16x8, make_uint4((x.x ^ sign) & some, (x.y ^ sign) & some, (x.z ^ sign) & some, (x.w ^ sign) & some));
     }
   }
-  __device__ __forceinline__ void scores(int used, const uint4 *k, pf_f32x4 (&sc)[NB][NT]) const {
+  // The values' fragments: of 16 dimensions dt, the rows 4 tq .. + 3 and those 16
+  // on (tr_frag).  In assembly with its own wait, since the builtin waits for the
+  // transfers of the next tile first.
+  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+  struct Values {
+    u32x2 lo[DT], hi[DT];
+  };
+  __device__ __forceinline__ static void read_values(const uint4 *v, int st, Values &f) {
+    const int lane = threadIdx.x & 63, ti = (lane & 15) >> 2, tg = lane & 3;
+    const int row = 4 * (lane >> 4) + ti;     // and the row 16 on, with the same swizzle
+    const uint32_t from = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)v + (32 * st + row) * L::RB + (tg & 1) * 8;
+    uint32_t at[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) at[dt] = from + ((2 * dt + (tg >> 1)) ^ L::vswz(row)) * 16;
+    static_assert(DT % 2 == 0, "two at a time");
+    if constexpr (DT % 4 == 0) {
+#pragma unroll
+      for (int dt = 0; dt < DT; dt += 4)
+        asm volatile(
+            "ds_read_b64_tr_b16 %0, %8\n ds_read_b64_tr_b16 %1, %8 offset:%12\n"
+            "ds_read_b64_tr_b16 %2, %9\n ds_read_b64_tr_b16 %3, %9 offset:%12\n"
+            "ds_read_b64_tr_b16 %4, %10\n ds_read_b64_tr_b16 %5, %10 offset:%12\n"
+            "ds_read_b64_tr_b16 %6, %11\n ds_read_b64_tr_b16 %7, %11 offset:%12\n"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(f.lo[dt]), "=&v"(f.hi[dt]), "=&v"(f.lo[dt + 1]), "=&v"(f.hi[dt + 1]), "=&v"(f.lo[dt + 2]),
+              "=&v"(f.hi[dt + 2]), "=&v"(f.lo[dt + 3]), "=&v"(f.hi[dt + 3])
+            : "v"(at[dt]), "v"(at[dt + 1]), "v"(at[dt + 2]), "v"(at[dt + 3]), "i"(16 * L::RB)
+            : "memory");
+    } else {
+      asm volatile(
+          "ds_read_b64_tr_b16 %0, %4\n ds_read_b64_tr_b16 %1, %4 offset:%6\n"
+          "ds_read_b64_tr_b16 %2, %5\n ds_read_b64_tr_b16 %3, %5 offset:%6\n"
+          "s_waitcnt lgkmcnt(0)"
+          : "=&v"(f.lo[0]), "=&v"(f.hi[0]), "=&v"(f.lo[1]), "=&v"(f.hi[1])
+          : "v"(at[0]), "v"(at[1]), "i"(16 * L::RB)
+          : "memory");
+    }
+  }
+  // (also asks for the first 32 values, to wait once)
+  __device__ __forceinline__ void scores(const uint4 *k, const uint4 *v, Values &f, pf_f32x4 (&sc)[NB][NT]) const {
     const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
+    const uint4 *from = k + r16 * CPR;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) sc[nb][nt] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
+    // 32 keys' fragments are asked for before their first product
 #pragma unroll
-    for (int st = 0; st < KS; ++st)
+    for (int t = 0; t < ST; ++t) {
+      pf_bf16x8 kf[KS][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int row = nt * 16 + r16;
-        const pf_bf16x8 kf = __builtin_bit_cast(pf_bf16x8, k[row * CPR + ((st * 4 + grp) ^ L::kswz(row))]);
+      for (int st = 0; st < KS; ++st)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          if (nb < used) sc[nb][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[nb][st], sc[nb][nt], 0, 0, 0);
-      }
+        for (int nt = 0; nt < 2; ++nt)      // (the swizzle is the same 16 rows on, so one address a k-step)
+          kf[st][nt] = __builtin_bit_cast(pf_bf16x8, from[(2 * t + nt) * 16 * CPR + ((st * 4 + grp) ^ L::kswz(r16))]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (t == ST - 1) read_values(v, 0, f);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int st = 0; st < KS; ++st)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            sc[nb][2 * t + nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[st][nt], q[nb][st], sc[nb][2 * t + nt], 0, 0, 0);
+    }
   }
-  // o += V^T P^T; ODD: without the values that are no finite numbers
-  template <bool ODD>
-  __device__ __forceinline__ void outputs(int used, const uint4 *v, const pf_f32x4 (&p)[NB][NT]) {
-    const int lane = threadIdx.x & 63, tq = lane >> 4, ti = (lane & 15) >> 2, tg = lane & 3;
-    pf_bf16x8 pp[NB][3];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
+  // Scores to weights e^(s - reference), in powers of two, whose sum joins l, and
+  // o += V^T P^T.  32 keys of a column block at a time: the vector work on one is
+  // laid between the products of the one before.
+  __device__ __forceinline__ void outputs(const uint4 *v, Values &f, pf_f32x4 (&sc)[NB][NT], float scale2, const float (&m)[NB],
+                                          float (&l)[NB]) {
+    constexpr int ALL = NB * ST;
+    pf_bf16x8 pp[2][3];
+    auto weights = [&](int nb, int st, pf_bf16x8 (&to)[3]) {
+      const float ref = m[nb] == -INFINITY ? 0.f : -m[nb];
+      float sum = 0.f;
       uint32_t part[3][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float a = p[nb][i / 2][2 * (i % 2)], b = p[nb][i / 2][2 * (i % 2) + 1];
+        float e[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          pf_f32x4 &x = sc[nb][2 * st + i / 2];
+          x[2 * (i % 2) + j] = e[j] = __builtin_amdgcn_exp2f(fmaf(x[2 * (i % 2) + j], scale2, ref));
+        }
+        sum += e[0] + e[1];
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
-          part[k][i] = upper_halves(a, b);
-          a = after_upper(a);
-          b = after_upper(b);
+          part[k][i] = k == 0 ? upper_halves(e[0], e[1]) : some_halves(upper_halves(e[0], e[1]));
+          e[0] = after_upper(e[0]);
+          e[1] = after_upper(e[1]);
         }
       }
+      l[nb] += sum;
 #pragma unroll
       for (int k = 0; k < 3; ++k)
-        pp[nb][k] = __builtin_bit_cast(pf_bf16x8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3]));
-    }
-    const uint16_t *base = (const uint16_t *)v;
-    const int lo = 4 * tq + ti, hi = lo + 16;
+        to[k] = __builtin_bit_cast(pf_bf16x8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3]));
+    };
+    weights(0, 0, pp[0]);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const int c = 2 * dt + (tg >> 1);
-      pf_bf16x8 vf = tr_frag(base + (lo * CPR + (c ^ L::vswz(lo))) * 8 + (tg & 1) * 4,
-                             base + (hi * CPR + (c ^ L::vswz(hi))) * 8 + (tg & 1) * 4);
-      if constexpr (ODD) {
-        uint4 x = __builtin_bit_cast(uint4, vf);
-        auto even = [](uint32_t w) {
-          if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
-          return (w & 0x7f800000u) == 0x7f800000u ? w & 0xffffu : w;
-        };
-        vf = __builtin_bit_cast(pf_bf16x8, make_uint4(even(x.x), even(x.y), even(x.z), even(x.w)));
+    for (int c = 0; c < ALL; ++c) {
+      const int nb = c % NB, st = c / NB;
+      if (nb == 0 && st > 0) read_values(v, st, f);
+      __builtin_amdgcn_sched_barrier(0);
+      if (c + 1 < ALL) weights((c + 1) % NB, (c + 1) / NB, pp[(c + 1) % 2]);
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const pf_bf16x8 vf = __builtin_bit_cast(pf_bf16x8, make_uint4(f.lo[dt].x, f.lo[dt].y, f.hi[dt].x, f.hi[dt].y));
+          o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[c % 2][k], o[nb][dt], 0, 0, 0);
+        }
+      if (c + 1 < ALL) {
+#pragma unroll
+        for (int i = 0; i < 3 * DT; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, DT == 8 ? 4 : DT == 4 ? 8 : 16, 0);
+        }
       }
-#pragma unroll
-      for (int k = 0; k < 3; ++k)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          if (nb < used) o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[nb][k], o[nb][dt], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // Element (key, d) of the values; whether a chunk of them holds one that is no finite number.
-  __device__ __forceinline__ static float value(const uint4 *v, int key, int d) {
-    const uint16_t *e = (const uint16_t *)v + (key * CPR + ((d / 8) ^ L::vswz(key))) * 8 + d % 8;
-    return __uint_as_float((uint32_t)*e << 16);
+  __device__ __forceinline__ static float value(const void *row, int d) {
+    return __uint_as_float((uint32_t)((const uint16_t *)row)[d] << 16);
   }
+  // Whether a chunk of values holds one that is no finite number; it without those.
   __device__ __forceinline__ static bool odd_chunk(const uint4 &x) {
     auto odd = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
     return odd(x.x) || odd(x.y) || odd(x.z) || odd(x.w);
+  }
+  __device__ __forceinline__ static uint4 even_chunk(const uint4 &x) {
+    auto even = [](uint32_t w) {
+      if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+      return (w & 0x7f800000u) == 0x7f800000u ? w & 0xffffu : w;
+    };
+    return make_uint4(even(x.x), even(x.y), even(x.z), even(x.w));
   }
   // four neighbouring dimensions of an output: which, and their values
   static constexpr int QUADS = DT;
@@ -215,12 +286,12 @@ struct Cols<uint16_t, HD, NB> {
 // fp32: a key lane holds dimensions 4 grp .. + 3 of each 16, so one 16-byte read
 // feeds four k-steps; a value lane holds W neighbouring dimensions of one key,
 // each the row of another 16-dimension tile.
-template <int HD, int NB>
-struct Cols<float, HD, NB> {
-  using L = Tile<float, HD>;
+template <typename L, int HD, int NB>
+struct Cols<L, float, HD, NB> {
   static constexpr int NT = L::NT, DT = L::DT, CPR = L::CPR, W = HD >= 64 ? 4 : 2, VB = HD / (16 * W);
   typedef __attribute__((ext_vector_type(W))) float vecw;
   pf_f32x4 q[NB][DT], o[NB][DT];
+  struct Values {};
 
   __device__ __forceinline__ void load_q(int nb, const float *src, bool whole, float scale) {
     const int grp = (threadIdx.x & 63) >> 4;
@@ -238,56 +309,68 @@ struct Cols<float, HD, NB> {
       q[nb][t] = scale < 0.f ? -x : scale != 0.f ? x : (pf_f32x4)0.f;
     }
   }
-  __device__ __forceinline__ void scores(int used, const uint4 *k, pf_f32x4 (&sc)[NB][NT]) const {
+  __device__ __forceinline__ void scores(const uint4 *k, const uint4 *, Values &, pf_f32x4 (&sc)[NB][NT]) const {
     const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
     // four sums of a quarter of the dimensions each: one sum of all rounds more
-    pf_f32x4 part[NB][4];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
+    for (int nt = 0; nt < NT; ++nt) {
+      pf_f32x4 part[NB][4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) part[nb][e] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-    for (int t = 0; t < DT; ++t) {
-      const pf_f32x4 kf = __builtin_bit_cast(pf_f32x4, k[r16 * CPR + ((4 * t + grp) ^ L::kswz(r16))]);
+        for (int e = 0; e < 4; ++e) part[nb][e] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int t = 0; t < DT; ++t) {
+        const pf_f32x4 kf = __builtin_bit_cast(pf_f32x4, k[(16 * nt + r16) * CPR + ((4 * t + grp) ^ L::kswz(r16))]);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          if (nb < used) part[nb][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], q[nb][t][e], part[nb][e], 0, 0, 0);
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            part[nb][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], q[nb][t][e], part[nb][e], 0, 0, 0);
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) sc[nb][nt] = (part[nb][0] + part[nb][1]) + (part[nb][2] + part[nb][3]);
     }
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) sc[nb][0] = (part[nb][0] + part[nb][1]) + (part[nb][2] + part[nb][3]);
   }
-  template <bool ODD>
-  __device__ __forceinline__ void outputs(int used, const uint4 *v, const pf_f32x4 (&p)[NB][NT]) {
+  __device__ __forceinline__ void outputs(const uint4 *v, Values &, pf_f32x4 (&sc)[NB][NT], float scale2, const float (&m)[NB],
+                                          float (&l)[NB]) {
     const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = 4 * grp + i;
-      const float *row = (const float *)(v + key * CPR) + r16 * W;
+    for (int nb = 0; nb < NB; ++nb) {
+      const float ref = m[nb] == -INFINITY ? 0.f : -m[nb];
+      float sum = 0.f;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sc[nb][nt][i] = __builtin_amdgcn_exp2f(fmaf(sc[nb][nt][i], scale2, ref));
+          sum += sc[nb][nt][i];
+        }
+      l[nb] += sum;
+    }
+#pragma unroll
+    for (int j = 0; j < 4 * NT; ++j) {
+      const int nt = j / 4, i = j % 4;
+      const float *row = (const float *)(v + (16 * nt + 4 * grp + i) * CPR) + r16 * W;
 #pragma unroll
       for (int b = 0; b < VB; ++b) {
-        vecw x = *(const vecw *)(row + b * 16 * W);
-        if constexpr (ODD) {
-#pragma unroll
-          for (int e = 0; e < W; ++e)
-            if ((__float_as_uint(x[e]) & 0x7f800000u) == 0x7f800000u) x[e] = 0.f;
-        }
+        const vecw x = *(const vecw *)(row + b * 16 * W);
 #pragma unroll
         for (int e = 0; e < W; ++e)
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
-            if (nb < used)
-              o[nb][b * W + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], p[nb][0][i], o[nb][b * W + e], 0, 0, 0);
+            o[nb][b * W + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], sc[nb][nt][i], o[nb][b * W + e], 0, 0, 0);
       }
     }
   }
-  __device__ __forceinline__ static float value(const uint4 *v, int key, int d) {
-    return ((const float *)(v + key * CPR))[d];
-  }
+  __device__ __forceinline__ static float value(const void *row, int d) { return ((const float *)row)[d]; }
   __device__ __forceinline__ static bool odd_chunk(const uint4 &x) {
     auto odd = [](uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; };
     return odd(x.x) || odd(x.y) || odd(x.z) || odd(x.w);
+  }
+  __device__ __forceinline__ static uint4 even_chunk(const uint4 &x) {
+    auto even = [](uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u ? 0u : w; };
+    return make_uint4(even(x.x), even(x.y), even(x.z), even(x.w));
   }
   static constexpr int QUADS = HD / 16;
   __device__ __forceinline__ static int dim(int j) {
@@ -350,18 +433,21 @@ __device__ __forceinline__ void landed() {
 template <typename T, int HD, int NB, int WC>
 struct Shape {
   static constexpr int NW = WC > 4 ? WC : 4, WK = NW / WC, COLS = 16 * NB * WC;
-  using L = Tile<T, HD>;
+  static constexpr int TK = sizeof(T) == 2 ? 32 : 16;
+  using L = Tile<T, HD, TK>;
   static constexpr int STEP = L::TK * WK;                    // keys of a step
   static constexpr int RING = 4 * L::BYTES;                  // a key group's two tiles of keys and values
   static constexpr int MEET = WK > 1 ? NW * 16 * NB * (HD + 4) * 4 : 0;
   static constexpr int LDS = RING * WK > MEET ? RING * WK : MEET;
 };
 
-template <typename T, int HD, int NB, int WC>
-__global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW)) void span_attn_kernel(SpanArgs a, SpanGrid g) {
+template <bool TREE, typename T, int HD, int NB, int WC>
+__global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW)) __attribute__((amdgpu_waves_per_eu(WC == 1 && HD * sizeof(T) > 128 ? 1 : 2)))
+void span_attn_kernel(SpanArgs a, SpanGrid g) {
   using S = Shape<T, HD, NB, WC>;
-  using L = Tile<T, HD>;
-  using C = Cols<T, HD, NB>;
+  using L = typename S::L;
+  using C = Cols<L, T, HD, NB>;
+  typedef std::conditional_t<(L::TK > 32), uint64_t, uint32_t> Bits;       // of a tile's keys
   constexpr int TK = L::TK, NT = L::NT, NW = S::NW, WK = S::WK;
   __shared__ __attribute__((aligned(16))) char lds[S::LDS];
   __shared__ float wm[NW][16 * NB], wl[NW][16 * NB];
@@ -382,45 +468,66 @@ __global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW)) void span_attn_ker
   const int first = split * plan.steps * S::STEP;
   const int steps = min(plan.steps, (sp.keys - first + S::STEP - 1) / S::STEP);
   const int c0 = (block * WC + wc) * 16 * NB;                // the wave's first column
-  const int used = min(NB, (cols - c0 + 15) / 16);           // its blocks with columns
   uint4 *ring = (uint4 *)(lds + wk * S::RING);
 
-  // the cache rows of a step's keys: lane j holds key j's
+  // The cache rows of a step's keys, lane j key j's, in three steps of which the
+  // loads have an iteration each to come back: the column, the page, the row.
   auto key_of = [&](int step) { return first + step * S::STEP + wk * TK; };
-  auto look = [&](int step) -> uint32_t {
-    if (step >= steps) return kNoRow;
-    const int slot = key_of(step) + (lane & (TK - 1));
-    if (slot >= sp.keys) return kNoRow;
-    int pos = slot;
-    if (a.columns != nullptr) {
-      const int c = a.columns[((size_t)b * kv + head) * a.n_cols + (slot >> a.map.shift)];
-      if (c < 0 || c >= a.map.max_pages) return kNoRow;
-      pos = (c << a.map.shift) + (slot & ((1 << a.map.shift) - 1));
-      if (pos >= sp.len) return kNoRow;
-    }
-    return page_row(a.map, sp.seq, pos, head);
+  auto slot_of = [&](int step) { return key_of(step) + (lane & (TK - 1)); };
+  auto column = [&](int step) -> int {
+    const int c = slot_of(step) >> a.map.shift;
+    if (TREE || a.columns == nullptr) return c;
+    return a.columns[((size_t)b * kv + head) * a.n_cols + min(c, a.n_cols - 1)];
   };
-  // a step's keys and values into the ring: transfer c moves rows RPT c ..;
-  // lane l fills chunk l % CPR of row RPT c + l / CPR with the swizzled one
+  auto is_column = [&](int step, int c) { return step < steps && slot_of(step) < sp.keys && c >= 0 && c < a.map.max_pages; };
+  auto page = [&](int step, int c) -> int { return a.map.table[is_column(step, c) ? (size_t)sp.seq * a.map.max_pages + c : 0]; };
+  auto row = [&](int step, int c, int p) -> uint32_t {
+    const int at = slot_of(step) & ((1 << a.map.shift) - 1);
+    const bool is = is_column(step, c) && p >= 0 && p < a.map.n_pages &&
+                    (TREE || a.columns == nullptr || (c << a.map.shift) + at < sp.len);
+    return is ? (((uint32_t)p * (uint32_t)kv + (uint32_t)head) << a.map.shift) + (uint32_t)at : kNoRow;
+  };
+  // A step's keys and values into the ring: transfer c moves rows RPT c ..; lane l
+  // fills chunk l % CPR of row RPT c + l / CPR with the swizzled one.  Where all
+  // keys are there and a transfer's rows lie in one page, its address is one
+  // scalar; otherwise a lane's, of zeros for keys that no row sees.
+  const bool runs = 1 << a.map.shift >= L::RPT;
+  const int l_row = lane / L::CPR, l_chunk = lane % L::CPR;
   auto issue = [&](int step, uint32_t rows) {
     uint4 *to = ring + (step & 1) * (2 * L::BYTES / 16);
-#pragma unroll
-    for (int t = 0; t < (L::NTR + WC - 1) / WC; ++t) {
-      const int c = t * WC + wc;
-      if (L::NTR % WC != 0 && c >= L::NTR) break;
-      const int row = c * L::RPT + lane / L::CPR, chunk = lane % L::CPR;
-      const uint32_t at = (uint32_t)__shfl((int)rows, row, 64);
-      const uint64_t off = (uint64_t)at * L::RB;
-      const char *kp = at == kNoRow ? (const char *)zero_row : (const char *)a.k + off;
-      const char *vp = at == kNoRow ? (const char *)zero_row : (const char *)a.v + off;
-      __builtin_amdgcn_global_load_lds((const void *)(kp + (chunk ^ L::kswz(row)) * 16),
-                                       (__attribute__((address_space(3))) void *)(to + c * 64), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const void *)(vp + (chunk ^ L::vswz(row)) * 16),
+    auto move = [&](int c, const char *kp, const char *vp) {
+      __builtin_amdgcn_global_load_lds((const void *)kp, (__attribute__((address_space(3))) void *)(to + c * 64), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const void *)vp,
                                        (__attribute__((address_space(3))) void *)(to + L::BYTES / 16 + c * 64), 16, 0, 0);
+    };
+    auto each = [&](auto address) {
+#pragma unroll
+      for (int t = 0; t < (L::NTR + WC - 1) / WC; ++t) {
+        const int c = t * WC + wc, row = c * L::RPT + l_row;
+        if (L::NTR % WC != 0 && c >= L::NTR) break;
+        address(c, row, (uint32_t)(l_chunk ^ L::kswz(row)) * 16, (uint32_t)(l_chunk ^ L::vswz(row)) * 16);
+      }
+    };
+    if (runs && __ballot(lane >= TK || rows != kNoRow) == ~0ull) {
+      each([&](int c, int, uint32_t kc, uint32_t vc) {
+        const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)rows, c * L::RPT) * L::RB;
+        move(c, (const char *)a.k + off + (uint32_t)(l_row * L::RB + kc), (const char *)a.v + off + (uint32_t)(l_row * L::RB + vc));
+      });
+    } else {
+      each([&](int c, int row, uint32_t kc, uint32_t vc) {
+        const uint32_t at = (uint32_t)__shfl((int)rows, row, 64);
+        const uint64_t off = (uint64_t)at * L::RB;
+        move(c, (at == kNoRow ? (const char *)zero_row : (const char *)a.k + off) + kc,
+             (at == kNoRow ? (const char *)zero_row : (const char *)a.v + off) + vc);
+      });
     }
   };
 
-  uint32_t rows = look(0), rows1 = look(1);
+  int c1 = column(0), c2 = column(1), p1 = page(0, c1);
+  uint32_t rows = row(0, c1, p1);
+  c1 = c2;
+  p1 = page(1, c1);
+  c2 = column(2);
   if (steps > 0) issue(0, rows);
   C w;
   float m[NB], l[NB];                     // reference (powers of two) and this lane's part of the sum
@@ -436,14 +543,26 @@ __global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW)) void span_attn_ker
   }
   const float scale2 = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;   // the query has the sign, or is 0
 
-  for (int step = 0; step < steps; ++step) {
-    const uint32_t rows2 = look(step + 2);
+  auto work = [&](int step, auto drafted) {
+    constexpr bool DRAFT = decltype(drafted)::value;         // the step may have drafted keys
+    const uint32_t rows1 = row(step + 1, c1, p1);
+    auto ask = [&] {                      // for the pages of the step after next
+      c1 = c2;
+      p1 = page(step + 2, c1);
+      c2 = column(step + 3);
+    };
     if constexpr (WC > 1) {
-      // the step has landed for every wave, and every wave is past the last
-      // one, whose place the next takes
+      // the step has landed for every wave, and every wave is past the last one,
+      // whose place the next takes; the pages come after the transfers, since
+      // this wait is for all that was asked for before (tree_8x64x8200: 174 us
+      // with them before it, 157 so)
       lds_ring_step<0>();
       if (step + 1 < steps) issue(step + 1, rows1);
+      ask();
+      __builtin_amdgcn_sched_barrier(0);
     } else {
+      // two steps' transfers on their way, for which the pages come first
+      ask();
       if (step + 1 < steps) {
         issue(step + 1, rows1);
         landed<2 * L::NTR>();
@@ -451,16 +570,33 @@ __global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW)) void span_attn_ker
         landed<0>();
       }
     }
-    const uint4 *k = ring + (step & 1) * (2 * L::BYTES / 16), *v = k + L::BYTES / 16;
+    uint4 *k = ring + (step & 1) * (2 * L::BYTES / 16), *v = k + L::BYTES / 16;
     const int key0 = key_of(step);
     const unsigned long long ballot = __ballot(lane < TK && rows != kNoRow);
-    const uint32_t there = (uint32_t)ballot;                 // keys that some row may see
-    constexpr uint32_t kAll = TK == 32 ? 0xffffffffu : 0xffffu;
-    const bool trees = a.mask != nullptr && key0 + TK > sp.len;
-    if (used > 0 && there != 0) {
+    const Bits there = (Bits)ballot;                         // keys that some row may see
+    constexpr Bits kAll = (Bits)(~0ull >> (64 - TK));
+    const bool trees = DRAFT && key0 + TK > sp.len;
+    Bits odd = 0;
+    if (DRAFT) {
+      // Drafted values that some rows see and others do not: 0 times an infinity
+      // or NaN is not 0, so those leave the tile and go by themselves.  (The same
+      // steps for all waves: they share tiles.)
+      for (int e = lane; e < TK * L::CPR; e += 64)
+        if (C::odd_chunk(v[e])) odd |= (Bits)1 << (e / L::CPR);
+#pragma unroll
+      for (int s = 1; s < 64; s <<= 1) odd |= (Bits)__shfl_xor((long long)odd, s, 64);
+      if constexpr (WC > 1) __syncthreads();
+      if (odd != 0) {
+        for (int e = lane; e < TK * L::CPR; e += 64) v[e] = C::even_chunk(v[e]);
+        wave_lds_sync();
+      }
+      if constexpr (WC > 1) __syncthreads();
+    }
+    if (c0 < cols && there != 0) {
       pf_f32x4 sc[NB][NT];
-      w.scores(used, k, sc);
-      uint32_t sees[NB];
+      typename C::Values f;
+      w.scores(k, v, f, sc);
+      Bits sees[NB];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) sees[nb] = there;
       if (trees) {
@@ -474,13 +610,13 @@ __global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW)) void span_attn_ker
           uint64_t x = at < a.words ? bits[at] >> sh : 0;
           if (sh > 0 && at + 1 < a.words) x |= bits[at + 1] << (64 - sh);
           if (d0 < 0) x = x << -d0 | ((1ull << -d0) - 1);    // (-d0 < TK)
-          sees[nb] &= (uint32_t)x;
+          sees[nb] &= (Bits)x;
         }
       }
       if (trees || there != kAll) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const uint32_t mine = sees[nb] >> (4 * grp);
+          const Bits mine = sees[nb] >> (4 * grp);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -488,7 +624,7 @@ __global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW)) void span_attn_ker
               if (!(mine >> (nt * 16 + i) & 1)) sc[nb][nt][i] = -INFINITY;
         }
       }
-      if (g.score != nullptr) {
+      if (!TREE && g.score != nullptr) {
         // (one row: a column is a head, and lies in block 0 .. NB - 1)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -525,61 +661,44 @@ __global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW)) void span_attn_ker
           for (int dt = 0; dt < C::DT; ++dt) w.o[nb][dt] *= shrink;
         }
       }
+      w.outputs(v, f, sc, scale2, m, l);
+      for (Bits left = odd; left != 0; left &= left - 1) {
+        const int key = __builtin_amdgcn_readfirstlane(__builtin_ctzll(left));
+        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)rows, key);
+        const char *from = (const char *)a.v + (uint64_t)at * L::RB;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const float ref = m[nb] == -INFINITY ? 0.f : -m[nb];
-        float sum = 0.f;
+        for (int nb = 0; nb < NB; ++nb) {
+          float p = 0.f;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(sc[nb][nt][i], scale2, ref));
-            sc[nb][nt][i] = p;
-            sum += p;
-          }
-        l[nb] += sum;
-      }
-      uint32_t bad = 0;
-      if (trees) {
-        // Drafted values that some rows see and others do not: 0 times an
-        // infinity or NaN is not 0, so those go by themselves.
-        for (int e = lane; e < TK * L::CPR; e += 64)
-          if (C::odd_chunk(v[e])) bad |= 1u << (e / L::CPR);
+            for (int i = 0; i < 4; ++i)
+              if (key / 16 == nt && key % 4 == i) p = sc[nb][nt][i];
+          p = fmaxf(__shfl(p, (key >> 2 & 3) * 16 + r16, 64), 0x1p-100f);
+          if (sees[nb] >> key & 1) {
 #pragma unroll
-        for (int s = 1; s < 64; s <<= 1) bad |= (uint32_t)__shfl_xor((int)bad, s, 64);
-        bad = (uint32_t)__builtin_amdgcn_readfirstlane((int)bad);
-      }
-      if (bad == 0) {
-        w.template outputs<false>(used, v, sc);
-      } else {
-        w.template outputs<true>(used, v, sc);
-        for (uint32_t left = bad; left != 0; left &= left - 1) {
-          const int key = __builtin_ctz(left);
+            for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            float p = 0.f;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (key / 16 == nt && key % 4 == i) p = sc[nb][nt][i];
-            p = fmaxf(__shfl(p, (key >> 2 & 3) * 16 + r16, 64), 0x1p-100f);
-            if (sees[nb] >> key & 1) {
-#pragma unroll
-              for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const float x = C::value(v, key, C::dim_of(dt, i));
-                  if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) w.o[nb][dt][i] += p * x;
-                }
-            }
+              for (int i = 0; i < 4; ++i) {
+                const float y = C::value(from, C::dim_of(dt, i));
+                if ((__float_as_uint(y) & 0x7f800000u) == 0x7f800000u) w.o[nb][dt][i] += p * y;
+              }
           }
         }
       }
     }
     wave_lds_sync();                      // the tile is read before anything takes its place
     rows = rows1;
-    rows1 = rows2;
+  };
+  // (a loop without what only drafted keys need: with it the registers do not
+  // suffice, and a spilled one's reload waits for the next tile's transfers)
+  int step = 0;
+  if constexpr (TREE) {
+    const int before = max(0, min(steps, (sp.len - first) / S::STEP));
+    for (; step < before; ++step) work(step, std::false_type());
+    for (; step < steps; ++step) work(step, std::true_type());
+  } else {
+    for (; step < steps; ++step) work(step, std::false_type());
   }
 
   // rows behind the drafted ones see nothing
@@ -701,8 +820,6 @@ __global__ __launch_bounds__(256) void span_weigh_kernel(SpanArgs a, SpanGrid g,
   }
 }
 
-// How many splits, at most: by the workgroups that the call has without any.
-int most_splits(int64_t workgroups) { return (int)std::min<int64_t>(64, std::max<int64_t>(1, 1024 / workgroups)); }
 
 struct SpanSizes {
   int blocks, smax, least, step;
@@ -716,10 +833,15 @@ SpanSizes sizes_of(int n, int draft, int n_heads, int n_kv_heads, int keys, bool
   const int cols = draft * (n_heads / n_kv_heads);
   z.blocks = (cols + S::COLS - 1) / S::COLS;
   z.step = S::STEP;
-  z.least = std::max(1, 256 / S::STEP);
-  const int64_t most = (int64_t)keys + (trees ? draft : 0);
-  z.smax = most_splits((int64_t)std::max(n, 1) * n_kv_heads * z.blocks);
-  z.smax = (int)std::min<int64_t>(z.smax, std::max<int64_t>(1, (most + z.step * z.least - 1) / (z.step * z.least)));
+  const int64_t most = (int64_t)keys + (trees ? draft : 0), items = (int64_t)std::max(n, 1) * n_kv_heads * z.blocks;
+  // Splits of 1024 keys or more, shorter only where they would be fewer than 512
+  // workgroups: 24 ragged trees of 25 take 100 us with 1024, 112 with 512, 158 with
+  // 2048; 8 x 64 x 8200 179, 196 and 162; 32 rows of 4000 keys 131, 160 and 114.  At
+  // most 4096 workgroups, 64 splits a sequence.
+  const int64_t least = std::min<int64_t>(1024, std::max<int64_t>(256, most * items / 512));
+  z.least = std::max<int>(1, (int)(least / S::STEP));
+  z.smax = (int)std::min<int64_t>(64, std::max<int64_t>(1, 4096 / items));
+  z.smax = (int)std::min<int64_t>(z.smax, std::max<int64_t>(1, (most + S::STEP - 1) / S::STEP / z.least));
   const size_t heads = (size_t)n * draft * n_heads;
   z.records = z.smax > 1 ? heads * z.smax * HD * sizeof(float) : 0;
   z.stats = z.smax > 1 || weigh ? heads * z.smax * sizeof(float2) : 0;
@@ -729,11 +851,11 @@ SpanSizes sizes_of(int n, int draft, int n_heads, int n_kv_heads, int keys, bool
   return z;
 }
 
-template <typename T, int HD, int NB, int WC>
+template <bool TREE, typename T, int HD, int NB, int WC>
 hipError_t go(const SpanArgs &a, hipStream_t s) {
   using S = Shape<T, HD, NB, WC>;
   const bool weigh = a.weight_out != nullptr;
-  const SpanSizes z = sizes_of<T, HD, NB, WC>(a.n, a.draft, a.n_heads, a.map.n_kv_heads, a.most, a.mask != nullptr, weigh);
+  const SpanSizes z = sizes_of<T, HD, NB, WC>(a.n, a.draft, a.n_heads, a.map.n_kv_heads, a.most, TREE, weigh);
   SpanGrid g{};
   g.blocks = z.blocks;
   g.smax = z.smax;
@@ -748,7 +870,7 @@ hipError_t go(const SpanArgs &a, hipStream_t s) {
   g.whole = whole(a.q, a.q_row, a.q_head) && whole(a.out, a.out_row, a.out_head);
   const int64_t grid = (int64_t)a.n * a.map.n_kv_heads * z.blocks * z.smax;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  span_attn_kernel<T, HD, NB, WC><<<(unsigned)grid, 64 * S::NW, 0, s>>>(a, g);
+  span_attn_kernel<TREE, T, HD, NB, WC><<<(unsigned)grid, 64 * S::NW, 0, s>>>(a, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (z.smax > 1) {
@@ -802,7 +924,10 @@ size_t span_work(int dtype, int n, int draft, int n_heads, int n_kv_heads, int h
 hipError_t launch_span(int dtype, const SpanArgs &a, hipStream_t s) {
   return by_type(dtype, a.head_dim, [&](auto t, auto hd) {
     return by_columns<decltype(t), hd.value>(a.draft * (a.n_heads / a.map.n_kv_heads), [&](auto nb, auto wc) {
-      return go<decltype(t), hd.value, nb.value, wc.value>(a, s);
+      // one row has at most 64 columns
+      if constexpr (wc.value < 4)
+        if (a.mask == nullptr) return go<false, decltype(t), hd.value, nb.value, wc.value>(a, s);
+      return a.mask == nullptr ? hipErrorInvalidValue : go<true, decltype(t), hd.value, nb.value, wc.value>(a, s);
     });
   });
 }
