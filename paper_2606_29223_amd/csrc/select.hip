@@ -108,28 +108,54 @@ __device__ __forceinline__ Row row_of(const SelectArgs &a, int r) {
   return x;
 }
 
-// LPR lanes a page, a lane N dimensions of its least and largest keys.
+// LPR lanes a page, a lane N dimensions of its least and largest keys.  A
+// workgroup asks for all its pages' bounds at once: the kernel is the latency of
+// the chain length, table, bounds, and their stream.
+constexpr int SCORE_EACH = 4;             // pages a lane
 template <typename T, int HD>
-__global__ __launch_bounds__(THREADS) void score_kernel(SelectArgs a, int stride, int per, int parts) {
+__global__ __launch_bounds__(THREADS) void score_kernel(SelectArgs a, int stride, int parts, bool whole) {
   constexpr int N = 16 / sizeof(T), LPR = HD / N, PAGES = THREADS / LPR;
   const int kv = a.map.n_kv_heads, G = a.n_heads / kv, row = blockIdx.x / parts, head = row % kv, r = row / kv;
   const Row x = row_of(a, r);
-  const int first = (blockIdx.x - row * parts) * per, end = min(first + per, x.columns);
-  if (first >= end) return;
+  const int first = (blockIdx.x - row * parts) * PAGES * SCORE_EACH + threadIdx.x / LPR;
+  if (first - (int)threadIdx.x / LPR >= x.columns) return;
   const int d = threadIdx.x % LPR;
+  Chunk<T> lo[SCORE_EACH], hi[SCORE_EACH];
+  bool there[SCORE_EACH];
+  int page[SCORE_EACH];
+#pragma unroll
+  for (int e = 0; e < SCORE_EACH; ++e) {
+    const int c = first + e * PAGES;
+    page[e] = a.map.table[(size_t)x.seq * a.map.max_pages + min(c, x.columns - 1)];
+    there[e] = c < x.columns && page[e] >= 0 && page[e] < a.map.n_pages;
+  }
+#pragma unroll
+  for (int e = 0; e < SCORE_EACH; ++e) {
+    const T *b = (const T *)a.bounds + ((size_t)(there[e] ? page[e] : 0) * kv + head) * 2 * HD + d * N;
+    lo[e].raw = *(const uint4 *)b;
+    hi[e].raw = *(const uint4 *)(b + HD);
+  }
   double up[N], down[N];                  // q+ and q-, of all the kv head's heads
 #pragma unroll
   for (int i = 0; i < N; ++i) up[i] = down[i] = 0.0;
   const T *src = (const T *)a.q + (int64_t)r * a.q_row + (int64_t)head * G * a.q_head + d * N;
-  for (int g = 0; g < G; ++g, src += a.q_head)
+  for (int g = 0; g < G; ++g, src += a.q_head) {
+    Chunk<T> q;
+    if (whole) {
+      q.raw = *(const uint4 *)src;
+    } else {
+      T t[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) t[i] = src[i];
+      __builtin_memcpy(&q.raw, t, 16);
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      float v;
-      if constexpr (sizeof(T) == 2) v = __uint_as_float((uint32_t)src[i] << 16);
-      else v = src[i];
+      const float v = q.get(i);
       up[i] += v < 0.f ? 0.f : v;         // (a NaN goes on in both)
       down[i] += v > 0.f ? 0.f : v;
     }
+  }
   // a part of 0 adds nothing, whatever the bound (0 times infinity is not 0)
   uint32_t some_up[N], some_down[N];
 #pragma unroll
@@ -138,69 +164,151 @@ __global__ __launch_bounds__(THREADS) void score_kernel(SelectArgs a, int stride
     some_down[i] = down[i] == 0.0 ? 0u : ~0u;
   }
   uint64_t *keys = (uint64_t *)a.work + (size_t)row * stride;
-  for (int c0 = first; c0 < end; c0 += PAGES) {
-    const int c = c0 + threadIdx.x / LPR;
-    int page = -1;
-    if (c < end) page = a.map.table[(size_t)x.seq * a.map.max_pages + c];
-    const bool there = page >= 0 && page < a.map.n_pages;
-    Chunk<T> lo, hi;
-    lo.raw = hi.raw = make_uint4(0, 0, 0, 0);
-    if (there) {
-      const T *b = (const T *)a.bounds + ((size_t)page * kv + head) * 2 * HD + d * N;
-      lo.raw = *(const uint4 *)b;
-      hi.raw = *(const uint4 *)(b + HD);
-    }
+#pragma unroll
+  for (int e = 0; e < SCORE_EACH; ++e) {
+    const int c = first + e * PAGES;
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float l = lo.get(i), h = hi.get(i);
+      const float l = lo[e].get(i), h = hi[e].get(i);
       const uint32_t least = __float_as_uint(l > h ? h : l), most = __float_as_uint(l > h ? l : h);
       sum = __builtin_fma(up[i], (double)__uint_as_float(most & some_up[i]), sum);
       sum = __builtin_fma(down[i], (double)__uint_as_float(least & some_down[i]), sum);
     }
 #pragma unroll
     for (int o = LPR / 2; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    if (d == 0 && c < end) {
+    if (d == 0 && c < x.columns) {
       const bool fixed = c < a.sinks || c >= x.columns - a.recent;
-      keys[c] = !there ? 0 : fixed ? ~0ull : order_of(sum);
+      keys[c] = !there[e] ? 0 : fixed ? ~0ull : order_of(sum);
     }
   }
 }
 
 // ----------------------------------------------------------- the n largest
-// The n largest of the keys 1 .. of places 0 .. count - 1, in ascending places;
-// the lowest places among equals.  take(place, rank, key) is called for each,
-// once all keys of its turn have been read.
-template <typename K>
+// The n largest of `count` keys, of equal ones those of the lowest places, in
+// ascending places.  A key of 0 is none, the largest one (all bits) is always
+// taken: the caller sees to it that no more than n have it.
+//
+// A workgroup keeps EACH neighbouring keys a lane, all of them where they are few
+// enough, and otherwise reads them again each time.  Keys of a row are alike in
+// their upper bits: the digits by which they are told apart begin at the first
+// bit in which the least and the largest differ.  Digit by digit, 8 bits a pass,
+// the bucket that holds the n-th largest narrows until it is taken whole.
+template <typename K, int TH>
 struct Pick {
-  int hist[256];
-  int before[THREADS / 64], ties[THREADS / 64];
+  int hist[TH / 64][256];                 // a wave's own: lanes of one wave alone meet in a bucket
+  K lo[TH / 64], hi[TH / 64];
+  int sum[TH / 64];
   K prefix;
-  int left, shift;
+  int left;
 };
 
-template <typename K, typename Key, typename Take>
-__device__ __forceinline__ int pick_largest(Pick<K> &s, int count, int n, Key key, Take take) {
-  constexpr int BITS = 8 * sizeof(K);
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v, int o) { return (uint32_t)__shfl_xor((int)v, o, 64); }
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int o) { return (uint64_t)__shfl_xor((long long)v, o, 64); }
+__device__ __forceinline__ int high_bits(uint32_t v) { return v == 0 ? 0 : 32 - __builtin_clz(v); }
+__device__ __forceinline__ int high_bits(uint64_t v) { return v == 0 ? 0 : 64 - __builtin_clzll(v); }
+
+// raw(place) is read for each place, key(raw, place) made of it; take(place, rank,
+// raw) is called for each that is taken, after all of its turn's raw were read.
+template <typename K, int TH, int EACH, typename Raw, typename Read, typename Key, typename Take>
+__device__ __forceinline__ int pick_largest(Pick<K, TH> &s, int count, int n, Read read, Key key, Take take) {
+  constexpr int TURN = TH * EACH, WAVES = TH / 64;
+  constexpr K kAlways = ~(K)0;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // digit by digit: of those that agree with the n-th largest so far, which
-  // digit it has next
-  K prefix = 0;
-  int left = n, shift = BITS;
-  while (shift > 0) {
-    s.hist[tid] = 0;
+  const bool once = count <= TURN;
+  Raw raw[EACH];
+  auto load = [&](int j0) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int j = j0 + tid * EACH + e;
+      raw[e] = read(j < count ? j : 0);
+    }
+  };
+  auto key_at = [&](int j0, int e) -> K {
+    const int j = j0 + tid * EACH + e;
+    return j < count ? key(raw[e], j) : 0;
+  };
+  auto turns = [&](auto f) {
+    for (int j0 = 0; j0 < count; j0 += TURN) {
+      if (!once) load(j0);
+      f(j0);
+    }
+  };
+  if (once && count > 0) load(0);
+  // how many are always taken, how many others there are, and their range
+  K lo = kAlways, hi = 0;
+  int fixed = 0, others = 0;
+  turns([&](int j0) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const K k = key_at(j0, e);
+      if (k == kAlways) ++fixed;
+      else if (k != 0) {
+        ++others;
+        lo = min(lo, k);
+        hi = max(hi, k);
+      }
+    }
+  });
+  auto all = [&](int v) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
     __syncthreads();
-    for (int j = tid; j < count; j += THREADS) {
-      const K k = key(j);
-      if (k != 0 && (shift == BITS || k >> (shift % BITS) == prefix)) atomicAdd(&s.hist[(int)(k >> (shift - 8)) & 255], 1);
+    if (lane == 0) s.sum[wave] = v;
+    __syncthreads();
+    int t = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) t += s.sum[w];
+    return t;
+  };
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    lo = min(lo, lane_xor(lo, o));
+    hi = max(hi, lane_xor(hi, o));
+  }
+  if (lane == 0) {
+    s.lo[wave] = lo;
+    s.hi[wave] = hi;
+  }
+  fixed = all(fixed);
+  others = all(others);
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    lo = min(lo, s.lo[w]);
+    hi = max(hi, s.hi[w]);
+  }
+  int left = min(n - fixed, others);      // to take of the others
+  // those above `floor` are taken, and of those that equal it above `shift` the
+  // first `left` (all, if `every`)
+  int shift = others > 0 ? high_bits((K)(lo ^ hi)) : 0;
+  K prefix = shift < (int)(8 * sizeof(K)) ? hi >> shift : 0;
+  bool every = left == others;
+  while (!every && left > 0 && shift > 0) {
+    const int bits = min(8, shift), next = shift - bits;
+    for (int i = tid; i < 256 * WAVES; i += TH) s.hist[i / 256][i % 256] = 0;
+    __syncthreads();
+    turns([&](int j0) {
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) {
+        const K k = key_at(j0, e);
+        if (k != 0 && k != kAlways && (shift == (int)(8 * sizeof(K)) || k >> shift == prefix))
+          atomicAdd(&s.hist[wave][(int)(k >> next) & ((1 << bits) - 1)], 1);
+      }
+    });
+    __syncthreads();
+    if (tid < 256) {
+      int sum = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) sum += s.hist[w][tid];
+      s.hist[0][tid] = sum;
     }
     __syncthreads();
-    // a lane a digit, the largest first: those with larger digits
+    // a lane four digits, the largest first: those with larger digits
     if (wave == 0) {
       int h[4], sum = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        h[i] = s.hist[255 - 4 * lane - i];
+        h[i] = s.hist[0][255 - 4 * lane - i];
         sum += h[i];
       }
       int upto = sum;
@@ -210,103 +318,99 @@ __device__ __forceinline__ int pick_largest(Pick<K> &s, int count, int n, Key ke
         if (lane >= o) upto += y;
       }
       int above = upto - sum;
-      const int all = __shfl(upto, 63, 64);
-      if (all <= left) {                  // all of them
-        if (lane == 0) s.left = -1;
-      } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (above < left && above + h[i] >= left) {
-            s.prefix = prefix << 8 | (K)(255 - 4 * lane - i);
-            s.left = above + h[i] == left ? 0 : left - above;
-          }
-          above += h[i];
+      for (int i = 0; i < 4; ++i) {
+        if (above < left && above + h[i] >= left) {
+          s.prefix = (shift == (int)(8 * sizeof(K)) ? 0 : prefix << bits) | (K)(255 - 4 * lane - i);
+          s.left = above + h[i] == left ? -1 : left - above;
         }
+        above += h[i];
       }
     }
     __syncthreads();
-    const int now = s.left;
-    if (now < 0) break;
     prefix = s.prefix;
-    shift -= 8;
-    left = now;
+    shift = next;
+    every = s.left < 0;
+    left = s.left;
     __syncthreads();
-    if (now == 0) break;
   }
-  // keys above the prefix, and of those that agree with it all (left 0, or no
-  // digit looked at) or the first `left`
-  const bool every = left == 0 || shift == BITS || s.left < 0;
+  // (no digit left to tell them apart: equal keys)
+  const bool whole_range = shift == (int)(8 * sizeof(K));    // every one of all is taken
   int done = 0, tied = 0;
-  for (int j0 = 0; j0 < count; j0 += THREADS) {
-    const int j = j0 + tid;
-    const K k = j < count ? key(j) : 0;
-    const K top = shift == BITS ? 0 : k >> (shift % BITS);
-    const bool same = k != 0 && top == prefix, above = k != 0 && top > prefix;
-    const unsigned long long ts = __ballot(same), as = __ballot(above);
-    if (lane == 0) {
-      s.ties[wave] = __popcll(ts);
-      s.before[wave] = __popcll(as);
-    }
-    __syncthreads();
-    int t = tied, a = done, all_t = tied, all_a = done;
+  turns([&](int j0) {
+    uint32_t same = 0, above = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-      if (w < wave) {
-        t += s.ties[w];
-        a += s.before[w];
+    for (int e = 0; e < EACH; ++e) {
+      const K k = key_at(j0, e), top = whole_range ? 0 : k >> shift;
+      if (k == kAlways) above |= 1u << e;
+      else if (k != 0) {
+        if (top == prefix) same |= 1u << e;
+        else if (top > prefix) above |= 1u << e;
       }
-      all_t += s.ties[w];
-      all_a += s.before[w];
     }
-    const unsigned long long under = (1ull << lane) - 1;
-    t += __popcll(ts & under);
-    a += __popcll(as & under);
-    // places before this one that are taken: a above, and of the ties
-    const bool mine = above || (same && (every || t < left));
-    if (mine) take(j, a + (every ? t : min(t, left)), k);
-    done = all_a;
-    tied = all_t;
+    // both counts in one number, 16 bits each
+    const int mine = __popc(same) << 16 | __popc(above);
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
+    }
     __syncthreads();
-  }
+    if (lane == 63) s.sum[wave] = upto;
+    __syncthreads();
+    int before = upto - mine, total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      if (w < wave) before += s.sum[w];
+      total += s.sum[w];
+    }
+    int a = done + (before & 0xffff), t = tied + (before >> 16);
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const bool is_same = same >> e & 1, is_above = above >> e & 1;
+      if (is_above || (is_same && (every || t < left))) take(j0 + tid * EACH + e, a + (every ? t : min(t, left)), raw[e]);
+      a += is_above;
+      t += is_same;
+    }
+    done += total & 0xffff;
+    tied += total >> 16;
+  });
   return done + (every ? tied : min(tied, left));
 }
 
-__global__ __launch_bounds__(THREADS) void select_kernel(SelectArgs a, int stride) {
-  __shared__ Pick<uint64_t> s;
+template <int TH, int EACH>
+__global__ __launch_bounds__(TH) void select_kernel(SelectArgs a, int stride) {
+  __shared__ Pick<uint64_t, TH> s;
   const Row x = row_of(a, blockIdx.x / a.map.n_kv_heads);
   const uint64_t *keys = (const uint64_t *)a.work + (size_t)blockIdx.x * stride;
   int *out = a.columns + (size_t)blockIdx.x * a.n_select;
-  const int n = pick_largest<uint64_t>(s, x.columns, a.n_select, [&](int j) { return keys[j]; },
-                                       [&](int j, int rank, uint64_t) { out[rank] = j; });
-  for (int i = n + threadIdx.x; i < a.n_select; i += THREADS) out[i] = -1;
+  const int n = pick_largest<uint64_t, TH, EACH, uint64_t>(
+      s, x.columns, a.n_select, [&](int j) { return keys[j]; }, [](uint64_t k, int) { return k; },
+      [&](int j, int rank, uint64_t) { out[rank] = j; });
+  for (int i = n + threadIdx.x; i < a.n_select; i += TH) out[i] = -1;
 }
 
-__global__ __launch_bounds__(THREADS) void evict_kernel(EvictArgs a) {
-  __shared__ Pick<uint32_t> s;
+// The weights follow their keys, in place too: a turn's are all read before the
+// first is written, and a place is never behind its source.
+template <int TH, int EACH>
+__global__ __launch_bounds__(TH) void evict_kernel(EvictArgs a) {
+  __shared__ Pick<uint32_t, TH> s;
   const int b = blockIdx.x / a.heads;
   const int len = max(0, min(a.len[b], a.capacity));
   const float *in = a.weight + (size_t)blockIdx.x * a.weight_ld;
   float *out = a.weight_out + (size_t)blockIdx.x * a.weight_out_ld;
   int *index = a.index + (size_t)blockIdx.x * a.budget;
-  const int n = pick_largest<uint32_t>(
-      s, len, a.budget,
-      [&](int j) { return j < a.sinks || j >= len - a.recent ? 0xffffffffu : order_of(in[j]); },
-      [&](int j, int rank, uint32_t) {
+  const int n = pick_largest<uint32_t, TH, EACH, float>(
+      s, len, a.budget, [&](int j) { return in[j]; },
+      [&](float w, int j) { return j < a.sinks || j >= len - a.recent ? ~0u : order_of(w); },
+      [&](int j, int rank, float w) {
         index[rank] = j;
+        out[rank] = w;
       });
   __syncthreads();
-  // the weights follow, turn by turn: a turn's are read before any is written,
-  // and a place is never behind its source
-  for (int j0 = 0; j0 < n; j0 += THREADS) {
-    const int j = j0 + threadIdx.x;
-    float w = 0.f;
-    if (j < n) w = in[index[j]];
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (j < n) out[j] = w;
-  }
-  for (int j = n + threadIdx.x; j < a.capacity; j += THREADS) out[j] = 0.f;
-  for (int i = n + threadIdx.x; i < a.budget; i += THREADS) index[i] = -1;
+  for (int j = n + threadIdx.x; j < a.capacity; j += TH) out[j] = 0.f;
+  for (int i = n + threadIdx.x; i < a.budget; i += TH) index[i] = -1;
   if (blockIdx.x % a.heads == 0 && threadIdx.x == 0) a.count[b] = n;
 }
 
@@ -339,11 +443,13 @@ size_t select_work(int n_rows, int n_kv_heads, int page_shift, int max_len) {
 hipError_t launch_select(int dtype, const SelectArgs &a, hipStream_t s) {
   const int columns = columns_of(a.map.shift, a.max_len), heads = a.n_rows * a.map.n_kv_heads;
   if (columns > 0) {
-    const int per = 128;
+    const int chunk = 16 / (dtype == DEX_F32 ? 4 : 2), per = THREADS / (a.head_dim / chunk) * SCORE_EACH;
     const int parts = (columns + per - 1) / per;
     const int64_t grid = (int64_t)parts * heads;
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
-#define DEX_SCORE(T, HD) score_kernel<T, HD><<<(unsigned)grid, THREADS, 0, s>>>(a, columns, per, parts)
+    const int64_t elem = dtype == DEX_F32 ? 4 : 2;
+    const bool whole = (uintptr_t)a.q % 16 == 0 && a.q_row * elem % 16 == 0 && a.q_head * elem % 16 == 0;
+#define DEX_SCORE(T, HD) score_kernel<T, HD><<<(unsigned)grid, THREADS, 0, s>>>(a, columns, parts, whole)
     if (dtype == DEX_F32) {
       if (a.head_dim == 32) DEX_SCORE(float, 32);
       else if (a.head_dim == 64) DEX_SCORE(float, 64);
@@ -357,12 +463,16 @@ hipError_t launch_select(int dtype, const SelectArgs &a, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  select_kernel<<<heads, THREADS, 0, s>>>(a, columns);
+  if (columns <= 2048) select_kernel<256, 8><<<heads, 256, 0, s>>>(a, columns);
+  else select_kernel<1024, 8><<<heads, 1024, 0, s>>>(a, columns);
   return hipGetLastError();
 }
 
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s) {
-  evict_kernel<<<a.n * a.heads, THREADS, 0, s>>>(a);
+  const int rows = a.n * a.heads;
+  if (a.capacity <= 1024) evict_kernel<256, 4><<<rows, 256, 0, s>>>(a);
+  else if (a.capacity <= 8192) evict_kernel<1024, 8><<<rows, 1024, 0, s>>>(a);
+  else evict_kernel<1024, 16><<<rows, 1024, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -74,52 +74,52 @@ __global__ __launch_bounds__(kMaxDraft) void tree_accept_kernel(TreeAcceptArgs a
   if (i < a.draft) a.path[at] = path[i];
 }
 
-// Entries of a (layer, sequence, kv head), a slice of their rows' 16-byte
-// chunks.  In place the entries go in turns: a turn's loads are all done before
-// its first store, and a source is never before its own destination, so it is
-// behind all earlier ones and no store overtakes a load.
+// Entries of `pairs` neighbouring (layer, kv head)s of a sequence, a slice of
+// their rows' 16-byte chunks.  In place the entries go in turns: a turn's loads
+// are all done before its first store, and a source is never before its own
+// destination, so it is behind all earlier ones and no store overtakes a load.
 constexpr int KEEP_THREADS = 256, KEEP_EACH = 8;
-__global__ __launch_bounds__(KEEP_THREADS) void keep_kernel(KeepArgs a, int lanes, int slices, int turns) {
+__global__ __launch_bounds__(KEEP_THREADS) void keep_kernel(KeepArgs a, int lanes, int slices, int pairs, int groups,
+                                                            int turns) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t chunk_t;
   const int kv = a.map.n_kv_heads;
   int x = blockIdx.x;
   const int slice = x % slices;
   x /= slices;
-  const int head = x % kv;
-  x /= kv;
-  const int layer = x % a.n_layers, s = x / a.n_layers;
+  const int pair0 = x % groups * pairs, s = x / groups, n_pairs = min(pairs, a.n_layers * kv - pair0);
   const int n = min(a.count[s], a.capacity);
   const int first = a.first != nullptr ? a.first[s] : 0;
-  const int chunk = slice * lanes + threadIdx.x % lanes, per = KEEP_THREADS / lanes, j_lane = threadIdx.x / lanes;
-  if (first < 0) return;
-  const int *index = a.index + layer * a.index_layer + s * a.index_seq + head * a.index_head;
+  if (first < 0 || n <= 0) return;
   const bool in_place = a.to == nullptr;
   PageMap to = a.map;
   if (!in_place) to.table = a.to, to.max_pages = a.to_pages;
-  const size_t base = (size_t)layer * a.map.n_pages * kv << a.map.shift;     // rows before the layer's
-  const bool mine = chunk * 16 < a.row_bytes && j_lane < per;
-  const int turn = per * KEEP_EACH;
-  const int j_first = blockIdx.y * turns * turn, j_end = min(n, j_first + turns * turn);
-  for (int j0 = j_first; j0 < j_end; j0 += turn) {
-    typedef __attribute__((ext_vector_type(4))) uint32_t chunk_t;
+  const size_t layer_rows = (size_t)a.map.n_pages * kv << a.map.shift;
+  // entries of the pairs one after the other, `per` of them a turn (a list of more
+  // than 256 has one pair)
+  const int per = KEEP_THREADS * KEEP_EACH / lanes, entries = n_pairs * n;
+  const int e_first = blockIdx.y * turns * per, e_end = min((int64_t)entries, (int64_t)e_first + (int64_t)turns * per);
+  for (int e0 = e_first; e0 < e_end; e0 += per) {
     chunk_t k[KEEP_EACH], v[KEEP_EACH];
     size_t dst[KEEP_EACH];
     bool go[KEEP_EACH];
 #pragma unroll
     for (int e = 0; e < KEEP_EACH; ++e) {
-      const int j = j0 + e * per + j_lane;
-      go[e] = mine && j < j_end;
+      const int item = e * KEEP_THREADS + threadIdx.x, in_turn = item / lanes, chunk = slice * lanes + item - in_turn * lanes;
+      const int entry = e0 + in_turn, in_pairs = pairs > 1 ? entry / n : 0, j = entry - in_pairs * n;
+      const int pair = pair0 + in_pairs, layer = pair / kv, head = pair - layer * kv;
+      go[e] = in_turn < per && entry < e_end && chunk * 16 < a.row_bytes;
       uint32_t from = kNoRow, into = kNoRow;
       if (go[e]) {
-        const int i = index[j];
+        const int i = a.index[layer * a.index_layer + s * a.index_seq + head * a.index_head + j];
         if (i >= 0 && i <= (1 << 30) && first <= (1 << 30) && !(in_place && i <= j)) {
           from = page_row(a.map, s, first + i, head);
           into = page_row(to, s, first + j, head);
         }
       }
       go[e] = from != kNoRow && into != kNoRow;
-      // (one that copies nothing reads the layer's first row)
-      const size_t src = (base + (go[e] ? from : 0)) * a.row_bytes + (mine ? chunk : 0) * 16;
-      dst[e] = (base + (go[e] ? into : 0)) * a.row_bytes + chunk * 16;
+      // (one that copies nothing reads the pools' first row)
+      const size_t at = layer * layer_rows, src = go[e] ? (at + from) * a.row_bytes + chunk * 16 : 0;
+      dst[e] = go[e] ? (at + into) * a.row_bytes + chunk * 16 : 0;
       k[e] = *(const chunk_t *)((const char *)a.k + src);
       v[e] = *(const chunk_t *)((const char *)a.v + src);
     }
@@ -136,21 +136,32 @@ __global__ __launch_bounds__(KEEP_THREADS) void keep_kernel(KeepArgs a, int lane
   }
 }
 
-// Pages behind a sequence's last token leave its row of the table.
+// Pages behind a sequence's last token leave its row of the table.  Small tables
+// go through one workgroup, which copies the counts first.
+constexpr int kTrimSmall = 16384, kTrimThreads = 1024;
+__device__ __forceinline__ void trim_entry(const TrimArgs &a, int64_t e) {
+  const int s = (int)(e / a.max_pages), c = (int)(e - (int64_t)s * a.max_pages);
+  int p = a.table[e];
+  if ((int64_t)c << a.shift >= max(0, a.len[s])) {
+    if (p >= 0 && p < a.n_pages) atomicSub(&a.ref_out[p], 1);
+    p = -1;
+  }
+  a.table_out[e] = p;
+}
+__global__ __launch_bounds__(kTrimThreads) void trim_small_kernel(TrimArgs a) {
+  if (a.ref_out != a.ref) {
+    for (int p = threadIdx.x; p < a.n_pages; p += kTrimThreads) a.ref_out[p] = a.ref[p];
+    __threadfence();                      // the counts are where the atomics see them
+    __syncthreads();
+  }
+  for (int e = threadIdx.x; e < a.n_seqs * a.max_pages; e += kTrimThreads) trim_entry(a, e);
+}
 __global__ __launch_bounds__(256) void trim_copy_kernel(TrimArgs a) {
   for (int p = blockIdx.x * 256 + threadIdx.x; p < a.n_pages; p += gridDim.x * 256) a.ref_out[p] = a.ref[p];
 }
 __global__ __launch_bounds__(256) void trim_kernel(TrimArgs a) {
   const int64_t entries = (int64_t)a.n_seqs * a.max_pages;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < entries; e += (int64_t)gridDim.x * 256) {
-    const int s = (int)(e / a.max_pages), c = (int)(e - (int64_t)s * a.max_pages);
-    int p = a.table[e];
-    if ((int64_t)c << a.shift >= max(0, a.len[s])) {
-      if (p >= 0 && p < a.n_pages) atomicSub(&a.ref_out[p], 1);
-      p = -1;
-    }
-    a.table_out[e] = p;
-  }
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < entries; e += (int64_t)gridDim.x * 256) trim_entry(a, e);
 }
 
 }  // namespace
@@ -166,17 +177,25 @@ hipError_t launch_tree_accept(const TreeAcceptArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_keep(const KeepArgs &a, hipStream_t s) {
-  const int chunks = a.row_bytes / 16;
-  const int lanes = std::min(chunks, 8), slices = (chunks + lanes - 1) / lanes;
-  const int turn = KEEP_THREADS / lanes * KEEP_EACH, all = (a.capacity + turn - 1) / turn;
-  const int64_t blocks = (int64_t)a.map.n_seqs * a.n_layers * a.map.n_kv_heads * slices;
+  const int chunks = a.row_bytes / 16, all = a.n_layers * a.map.n_kv_heads;
+  // short lists (a tree's path) take several pairs a workgroup; long ones in place
+  // are slices of 128 bytes, so that more workgroups go through them in turns
+  const bool in_place = a.to == nullptr, brief = a.capacity <= 256;
+  const int lanes = !in_place || brief ? chunks : std::min(chunks, 8), slices = (chunks + lanes - 1) / lanes;
+  const int pairs = brief ? std::min(all, 8) : 1, groups = (all + pairs - 1) / pairs;
+  const int64_t blocks = (int64_t)a.map.n_seqs * groups * slices;
+  const int per = KEEP_THREADS * KEEP_EACH / lanes, most = (int)(((int64_t)pairs * a.capacity + per - 1) / per);
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  const int split = a.to == nullptr ? 1 : std::min(all, 65535), turns = (all + split - 1) / split;
-  keep_kernel<<<dim3((unsigned)blocks, split), KEEP_THREADS, 0, s>>>(a, lanes, slices, turns);
+  const int split = in_place ? 1 : std::min(most, 65535), turns = (most + split - 1) / split;
+  keep_kernel<<<dim3((unsigned)blocks, split), KEEP_THREADS, 0, s>>>(a, lanes, slices, pairs, groups, turns);
   return hipGetLastError();
 }
 
 hipError_t launch_trim(const TrimArgs &a, hipStream_t s) {
+  if (a.n_pages <= kTrimSmall && (int64_t)a.n_seqs * a.max_pages <= kTrimSmall) {
+    trim_small_kernel<<<1, kTrimThreads, 0, s>>>(a);
+    return hipGetLastError();
+  }
   hipError_t e = hipSuccess;
   if (a.ref_out != a.ref) {
     trim_copy_kernel<<<std::min((a.n_pages + 255) / 256, 1024), 256, 0, s>>>(a);
