@@ -637,23 +637,25 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
         }
       }
       // A column's reference is raised, and its sums rescaled, only once a score
-      // exceeds it by 2^8, which leaves every rounding relative.
+      // exceeds it by 2^8, which leaves every rounding relative.  Each lane looks at
+      // its own scores; the four of a column meet where one of them calls for it.
       float mx[NB];
       bool up = false;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        float m0 = -INFINITY;
+        mx[nb] = -INFINITY;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) m0 = fmaxf(m0, sc[nb][nt][i]);
-        mx[nb] = quarters_max(m0) * scale2;
+          for (int i = 0; i < 4; ++i) mx[nb] = fmaxf(mx[nb], sc[nb][nt][i]);
+        mx[nb] *= scale2;
         up |= mx[nb] > m[nb] + 8.f;
       }
       if (__any(up)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const float now = mx[nb] > m[nb] + 8.f ? mx[nb] : m[nb];
+          const float top = quarters_max(mx[nb]);
+          const float now = top > m[nb] + 8.f ? top : m[nb];
           const float shrink = now == m[nb] ? 1.f : __builtin_amdgcn_exp2f(m[nb] - now);
           m[nb] = now;
           l[nb] *= shrink;
@@ -890,13 +892,17 @@ hipError_t go(const SpanArgs &a, hipStream_t s) {
   return e;
 }
 
-// The columns a workgroup takes: as many as the call has, so that keys are read
-// by few.
-template <typename T, int HD, typename F>
-auto by_columns(int cols, F f) {
+// Column blocks a wave, and neighbouring waves over the same keys.  A wave that
+// shares its tiles with others reads them from LDS for few columns, but has more
+// transfers on their way for its size: 8 trees of 8200 keys with their
+// columns in one block a wave and two: 24 columns 61 and 70 us, 32 61 and 70, 64 66
+// and 74, 128 113 and 92.  A few workgroups alone take the smaller blocks: one tree of 64 x 8200 39
+// us for 47.
+template <typename F>
+auto by_columns(int cols, int64_t pairs, F f) {
   if (cols <= 16) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-  if (cols <= 32) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
-  if (cols <= 64) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
+  if (cols <= 32) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
+  if (cols <= 64 || pairs * ((cols + 127) / 128) <= 32) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
   return f(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
 }
 template <typename F>
@@ -914,7 +920,7 @@ auto by_type(int dtype, int head_dim, F f) {
 
 size_t span_work(int dtype, int n, int draft, int n_heads, int n_kv_heads, int head_dim, int most, bool trees, bool weigh) {
   return by_type(dtype, head_dim, [&](auto t, auto hd) {
-    return by_columns<decltype(t), hd.value>(draft * (n_heads / n_kv_heads), [&](auto nb, auto wc) {
+    return by_columns(draft * (n_heads / n_kv_heads), (int64_t)n * n_kv_heads, [&](auto nb, auto wc) {
       const SpanSizes z = sizes_of<decltype(t), hd.value, nb.value, wc.value>(n, draft, n_heads, n_kv_heads, most, trees, weigh);
       return z.records + z.stats + z.scores;
     });
@@ -923,9 +929,9 @@ size_t span_work(int dtype, int n, int draft, int n_heads, int n_kv_heads, int h
 
 hipError_t launch_span(int dtype, const SpanArgs &a, hipStream_t s) {
   return by_type(dtype, a.head_dim, [&](auto t, auto hd) {
-    return by_columns<decltype(t), hd.value>(a.draft * (a.n_heads / a.map.n_kv_heads), [&](auto nb, auto wc) {
-      // one row has at most 64 columns
-      if constexpr (wc.value < 4)
+    return by_columns(a.draft * (a.n_heads / a.map.n_kv_heads), (int64_t)a.n * a.map.n_kv_heads, [&](auto nb, auto wc) {
+      // one row has at most 64 columns, in blocks of 16 a wave
+      if constexpr (nb.value == 1)
         if (a.mask == nullptr) return go<false, decltype(t), hd.value, nb.value, wc.value>(a, s);
       return a.mask == nullptr ? hipErrorInvalidValue : go<true, decltype(t), hd.value, nb.value, wc.value>(a, s);
     });
