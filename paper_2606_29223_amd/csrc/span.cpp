@@ -229,7 +229,7 @@ dex_status dex_pages_bounds(int32_t dtype, int32_t head_dim, const void *k_pages
   REFUSE_IF(n_new < 0, "n_new is below 0");
   const int64_t most = (int64_t)max_pages * page_size;
   if (n_new > most) n_new = (int32_t)most;
-  REFUSE_IF(((int64_t)n_new / page_size + 2) * n_kv_heads * n_seqs > (1ll << 31), "too many pages for one call");
+  REFUSE_IF(((int64_t)n_new / page_size + 2) * n_kv_heads * n_seqs > (1ll << 30), "too many pages for one call");
   if (n_new == 0) return DEX_OK;
   REFUSE_IF(!k_pages || !table || !length || !bounds, "an array is NULL");
   REFUSE_IF(!aligned(k_pages, 16) || !aligned(bounds, 16), "the pages or their bounds are not 16-byte aligned");

@@ -158,3 +158,20 @@ def test_weights_that_are_not_finite_and_lengths_out_of_range():
         got = paged.evict(w, ints(lens), budget, sinks=2, recent=3, weight_out=out)
         assert np.array_equal(host(got[0]), want[0]) and np.array_equal(host(got[1]), want[1])
         assert np.array_equal(host(out), want[2], equal_nan=True)
+
+
+@pytest.mark.parametrize("cap,lens,budget", [(40000, [40000, 16385, 100], 9001), (20000, [16384, 20000], 16384)])
+def test_long_evictions(cap, lens, budget):
+    """More keys than a workgroup holds at once, in place and not."""
+    torch = torch_cuda()
+    from paper_2606_29223_amd import paged
+    rng = np.random.default_rng(cap)
+    w = torch.from_numpy((rng.random((len(lens), 2, cap)) ** 4).astype(np.float32)).cuda()
+    w[:, 1] = (w[:, 1] * 64).floor()
+    want = ref.evict(host(w), lens, budget, 5, 77)
+    out = torch.full_like(w, 7.0)
+    got = paged.evict(w, ints(lens), budget, sinks=5, recent=77, weight_out=out)
+    assert np.array_equal(host(got[0]), want[0]) and np.array_equal(host(got[1]), want[1])
+    assert np.array_equal(host(out), want[2])
+    paged.evict(w, ints(lens), budget, sinks=5, recent=77)
+    assert np.array_equal(host(w), want[2])

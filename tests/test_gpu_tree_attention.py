@@ -177,6 +177,44 @@ def test_non_finite_keys_and_values_that_only_some_rows_see(dtype, draft):
         c.k[page, :, slot] = old
 
 
+@pytest.mark.parametrize("draft", [1, 6, 40])
+def test_infinite_values_before_the_tree(draft):
+    """Every row sees them: infinite of one sign, NaN for both."""
+    torch_cuda()
+    c = Case(draft, "bf16", 64, 8, 2, 16, [300, 90], draft)
+    for b, at in ((0, 250), (1, 3)):
+        c.v[int(c.table[b, at // 16]), :, at % 16, 4] = float("-inf")
+        c.v[int(c.table[b, at // 16]), :, at % 16, 9] = float("inf")
+        c.v[int(c.table[b, (at + 1) // 16]), :, (at + 1) % 16, 9] = float("-inf")
+    got, clean = host(c.run()[0]), c.want()[0]
+    assert np.isneginf(got[..., 4]).all() and np.isnan(got[..., 9]).all()
+    assert np.isfinite(np.delete(got, (4, 9), 2)).all() and clean.shape == got.shape
+
+
+def test_offsets_past_32_bits():
+    """Pages behind more than 2^32 elements of a layer."""
+    torch = torch_cuda()
+    from paper_2606_29223_amd import paged
+    c = Case(41, "bf16", 128, 4, 1, 1024, [1500, 40], 5)
+    n = (1 << 32) // (1024 * 128) + 8
+    k, v = (torch.empty((n, 1, 1024, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    far = np.where(c.table >= 0, c.table + n - len(c.k64), -1)
+    k[n - len(c.k64):], v[n - len(c.k64):] = c.k, c.v
+    want = [host(t) for t in c.run()]
+    mask = torch.from_numpy(ref.words(c.seen)).cuda()
+    got = paged.tree_attention(c.q, k, v, ints(far), ints(c.lens), mask, return_lse=True)
+    assert all(np.array_equal(a, host(b)) for a, b in zip(want, got))
+    # the same tokens moved, and their bounds
+    bounds = paged.page_bounds(k, ints(far), ints(c.lens))
+    near = paged.page_bounds(c.k, ints(c.table), ints(c.lens))
+    assert torch.equal(bounds[n - len(c.k64):], near)
+    index = ints(np.tile(np.arange(0, 1400, 2), (2, 1)))
+    count = ints([700, 20])
+    paged.keep(k[None], v[None], ints(far), index, count)
+    paged.keep(c.k[None], c.v[None], ints(c.table), index, count)
+    assert torch.equal(k[n - len(c.k64):], c.k) and torch.equal(v[n - len(c.k64):], c.v)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strided_and_unaligned_queries_and_outputs(dtype):
     torch = torch_cuda()
