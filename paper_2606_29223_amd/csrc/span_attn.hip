@@ -22,12 +22,14 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 __device__ uint4 zero_row[32];
 
 // How the keys of a sequence are cut: `n` splits of `steps` steps, a step being
-// a tile for each of a workgroup's key groups.
+// a tile for each of a workgroup's key groups, at most a quarter longer than
+// `least` steps while there are fewer than `smax`.
 struct SpanPlan {
   int steps, n;
 };
+__host__ __device__ __forceinline__ int splits_of(int steps, int least) { return max(1, (steps + least - 1 - least / 4) / least); }
 __host__ __device__ __forceinline__ SpanPlan span_plan(int keys, int step_keys, int smax, int least) {
-  const int all = (keys + step_keys - 1) / step_keys, n = max(1, min(smax, all / least));
+  const int all = (keys + step_keys - 1) / step_keys, n = min(smax, splits_of(all, least));
   SpanPlan p;
   p.steps = max(1, (all + n - 1) / n);
   p.n = max(1, (all + p.steps - 1) / p.steps);
@@ -114,7 +116,8 @@ struct Cols;
 
 template <typename L, int HD, int NB>
 struct Cols<L, uint16_t, HD, NB> {
-  static constexpr int KS = HD / 32, NT = L::NT, ST = NT / 2, DT = L::DT, CPR = L::CPR;
+  static constexpr int KS = HD / 32, NT = L::NT, DT = L::DT, CPR = L::CPR;
+  static_assert(NT == 2, "the keys of one product of the values");
   pf_bf16x8 q[NB][KS];
   pf_f32x4 o[NB][DT];
 
@@ -144,10 +147,10 @@ struct Cols<L, uint16_t, HD, NB> {
   struct Values {
     u32x2 lo[DT], hi[DT];
   };
-  __device__ __forceinline__ static void read_values(const uint4 *v, int st, Values &f) {
+  __device__ __forceinline__ static void read_values(const uint4 *v, Values &f) {
     const int lane = threadIdx.x & 63, ti = (lane & 15) >> 2, tg = lane & 3;
     const int row = 4 * (lane >> 4) + ti;     // and the row 16 on, with the same swizzle
-    const uint32_t from = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)v + (32 * st + row) * L::RB + (tg & 1) * 8;
+    const uint32_t from = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)v + row * L::RB + (tg & 1) * 8;
     uint32_t at[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) at[dt] = from + ((2 * dt + (tg >> 1)) ^ L::vswz(row)) * 16;
@@ -175,43 +178,37 @@ struct Cols<L, uint16_t, HD, NB> {
           : "memory");
     }
   }
-  // (also asks for the first 32 values, to wait once)
+  // (also asks for the values, to wait once)
   __device__ __forceinline__ void scores(const uint4 *k, const uint4 *v, Values &f, pf_f32x4 (&sc)[NB][NT]) const {
     const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
     const uint4 *from = k + r16 * CPR;
+    // all fragments are asked for before the first product
+    pf_bf16x8 kf[KS][2];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
+    for (int st = 0; st < KS; ++st)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) sc[nb][nt] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
-    // 32 keys' fragments are asked for before their first product
+      for (int nt = 0; nt < 2; ++nt)        // (the swizzle is the same 16 rows on, so one address a k-step)
+        kf[st][nt] = __builtin_bit_cast(pf_bf16x8, from[nt * 16 * CPR + ((st * 4 + grp) ^ L::kswz(r16))]);
+    __builtin_amdgcn_sched_barrier(0);
+    read_values(v, f);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int t = 0; t < ST; ++t) {
-      pf_bf16x8 kf[KS][2];
+    for (int nb = 0; nb < NB; ++nb) sc[nb][0] = sc[nb][1] = pf_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int st = 0; st < KS; ++st)
+    for (int st = 0; st < KS; ++st)
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt)      // (the swizzle is the same 16 rows on, so one address a k-step)
-          kf[st][nt] = __builtin_bit_cast(pf_bf16x8, from[(2 * t + nt) * 16 * CPR + ((st * 4 + grp) ^ L::kswz(r16))]);
-      __builtin_amdgcn_sched_barrier(0);
-      if (t == ST - 1) read_values(v, 0, f);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-      for (int st = 0; st < KS; ++st)
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-            sc[nb][2 * t + nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[st][nt], q[nb][st], sc[nb][2 * t + nt], 0, 0, 0);
-    }
+        for (int nb = 0; nb < NB; ++nb)
+          sc[nb][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[st][nt], q[nb][st], sc[nb][nt], 0, 0, 0);
   }
   // Scores to weights e^(s - reference), in powers of two, whose sum joins l, and
-  // o += V^T P^T.  32 keys of a column block at a time: the vector work on one is
-  // laid between the products of the one before.
-  __device__ __forceinline__ void outputs(const uint4 *v, Values &f, pf_f32x4 (&sc)[NB][NT], float scale2, const float (&m)[NB],
+  // o += V^T P^T.  A column block at a time: the vector work on one is laid
+  // between the products of the one before.
+  __device__ __forceinline__ void outputs(const uint4 *, Values &f, pf_f32x4 (&sc)[NB][NT], float scale2, const float (&m)[NB],
                                           float (&l)[NB]) {
-    constexpr int ALL = NB * ST;
     pf_bf16x8 pp[2][3];
-    auto weights = [&](int nb, int st, pf_bf16x8 (&to)[3]) {
+    auto weights = [&](int nb, pf_bf16x8 (&to)[3]) {
       const float ref = m[nb] == -INFINITY ? 0.f : -m[nb];
       float sum = 0.f;
       uint32_t part[3][4];
@@ -220,7 +217,7 @@ struct Cols<L, uint16_t, HD, NB> {
         float e[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          pf_f32x4 &x = sc[nb][2 * st + i / 2];
+          pf_f32x4 &x = sc[nb][i / 2];
           x[2 * (i % 2) + j] = e[j] = __builtin_amdgcn_exp2f(fmaf(x[2 * (i % 2) + j], scale2, ref));
         }
         sum += e[0] + e[1];
@@ -236,21 +233,19 @@ struct Cols<L, uint16_t, HD, NB> {
       for (int k = 0; k < 3; ++k)
         to[k] = __builtin_bit_cast(pf_bf16x8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3]));
     };
-    weights(0, 0, pp[0]);
+    weights(0, pp[0]);
 #pragma unroll
-    for (int c = 0; c < ALL; ++c) {
-      const int nb = c % NB, st = c / NB;
-      if (nb == 0 && st > 0) read_values(v, st, f);
+    for (int nb = 0; nb < NB; ++nb) {
       __builtin_amdgcn_sched_barrier(0);
-      if (c + 1 < ALL) weights((c + 1) % NB, (c + 1) / NB, pp[(c + 1) % 2]);
+      if (nb + 1 < NB) weights(nb + 1, pp[(nb + 1) % 2]);
 #pragma unroll
       for (int k = 0; k < 3; ++k)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
           const pf_bf16x8 vf = __builtin_bit_cast(pf_bf16x8, make_uint4(f.lo[dt].x, f.lo[dt].y, f.hi[dt].x, f.hi[dt].y));
-          o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[c % 2][k], o[nb][dt], 0, 0, 0);
+          o[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[nb % 2][k], o[nb][dt], 0, 0, 0);
         }
-      if (c + 1 < ALL) {
+      if (nb + 1 < NB) {
 #pragma unroll
         for (int i = 0; i < 3 * DT; ++i) {
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -429,10 +424,12 @@ __device__ __forceinline__ void landed() {
 }
 
 // The waves of a workgroup: WC neighbouring column blocks over the same keys,
-// WK = NW / WC groups of keys.
+// WK = NW / WC groups of keys.  Alone, bf16 waves go by two, since four have 128
+// KB of tiles and one workgroup on a CU, which then waits for the first of them:
+// 32 ragged rows' weights 78 us with four, 74 with two.
 template <typename T, int HD, int NB, int WC>
 struct Shape {
-  static constexpr int NW = WC > 4 ? WC : 4, WK = NW / WC, COLS = 16 * NB * WC;
+  static constexpr int NW = WC > 1 || sizeof(T) == 4 ? 4 : 2, WK = NW / WC, COLS = 16 * NB * WC;
   static constexpr int TK = sizeof(T) == 2 ? 32 : 16;
   using L = Tile<T, HD, TK>;
   static constexpr int STEP = L::TK * WK;                    // keys of a step
@@ -447,7 +444,6 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
   using S = Shape<T, HD, NB, WC>;
   using L = typename S::L;
   using C = Cols<L, T, HD, NB>;
-  typedef std::conditional_t<(L::TK > 32), uint64_t, uint32_t> Bits;       // of a tile's keys
   constexpr int TK = L::TK, NT = L::NT, NW = S::NW, WK = S::WK;
   __shared__ __attribute__((aligned(16))) char lds[S::LDS];
   __shared__ float wm[NW][16 * NB], wl[NW][16 * NB];
@@ -461,7 +457,9 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
   x /= kv;
   const int block = x % g.blocks;
   x /= g.blocks;
-  const int b = x % a.n, split = x / a.n;
+  // (turned on by one each split: workgroups go to the XCD's parts in turn, and
+  // the splits of a long sequence would all go to one: 24 ragged trees 102 us for 90)
+  const int split = x / a.n, b = (x + split) % a.n;
   const Span sp = span_of(a, b);
   const SpanPlan plan = span_plan(sp.keys, S::STEP, g.smax, g.least);
   if (split >= plan.n) return;
@@ -470,21 +468,27 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
   const int c0 = (block * WC + wc) * 16 * NB;                // the wave's first column
   uint4 *ring = (uint4 *)(lds + wk * S::RING);
 
-  // The cache rows of a step's keys, lane j key j's, in three steps of which the
-  // loads have an iteration each to come back: the column, the page, the row.
+  // The cache rows of a step's keys, lane j key j's.  The pages of 64 columns are
+  // held, lane j the j-th's, so that between the transfers there is hardly ever a
+  // load to wait for: a wait is for all that was asked for before.
   auto key_of = [&](int step) { return first + step * S::STEP + wk * TK; };
-  auto slot_of = [&](int step) { return key_of(step) + (lane & (TK - 1)); };
-  auto column = [&](int step) -> int {
-    const int c = slot_of(step) >> a.map.shift;
-    if (TREE || a.columns == nullptr) return c;
-    return a.columns[((size_t)b * kv + head) * a.n_cols + min(c, a.n_cols - 1)];
+  int held = 0, page = -1, column = 0;    // column of lane 0; this lane's page and column
+  auto hold = [&](int step) {
+    held = key_of(step) >> a.map.shift;
+    column = held + lane;
+    bool is = column <= (sp.keys - 1) >> a.map.shift;        // (no keys, nothing is read: the sequence may be none)
+    if (!TREE && a.columns != nullptr) column = a.columns[((size_t)b * kv + head) * a.n_cols + (is ? column : 0)];
+    is = is && column >= 0 && column < a.map.max_pages;
+    page = a.map.table[is ? (size_t)sp.seq * a.map.max_pages + column : 0];
+    if (!is || page >= a.map.n_pages) page = -1;
   };
-  auto is_column = [&](int step, int c) { return step < steps && slot_of(step) < sp.keys && c >= 0 && c < a.map.max_pages; };
-  auto page = [&](int step, int c) -> int { return a.map.table[is_column(step, c) ? (size_t)sp.seq * a.map.max_pages + c : 0]; };
-  auto row = [&](int step, int c, int p) -> uint32_t {
-    const int at = slot_of(step) & ((1 << a.map.shift) - 1);
-    const bool is = is_column(step, c) && p >= 0 && p < a.map.n_pages &&
-                    (TREE || a.columns == nullptr || (c << a.map.shift) + at < sp.len);
+  auto row = [&](int step) -> uint32_t {
+    if (step >= steps) return kNoRow;
+    const int key0 = key_of(step);
+    if (((key0 + TK - 1) >> a.map.shift) - held >= 64) hold(step);
+    const int key = key0 + (lane & (TK - 1)), at = key & ((1 << a.map.shift) - 1), j = (key >> a.map.shift) - held;
+    const int p = __shfl(page, j, 64), c = TREE || a.columns == nullptr ? 0 : __shfl(column, j, 64);    // (of all lanes)
+    const bool is = key < sp.keys && p >= 0 && (TREE || a.columns == nullptr || (c << a.map.shift) + at < sp.len);
     return is ? (((uint32_t)p * (uint32_t)kv + (uint32_t)head) << a.map.shift) + (uint32_t)at : kNoRow;
   };
   // A step's keys and values into the ring: transfer c moves rows RPT c ..; lane l
@@ -523,11 +527,8 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
     }
   };
 
-  int c1 = column(0), c2 = column(1), p1 = page(0, c1);
-  uint32_t rows = row(0, c1, p1);
-  c1 = c2;
-  p1 = page(1, c1);
-  c2 = column(2);
+  hold(0);
+  uint32_t rows = row(0);
   if (steps > 0) issue(0, rows);
   C w;
   float m[NB], l[NB];                     // reference (powers of two) and this lane's part of the sum
@@ -545,46 +546,33 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
 
   auto work = [&](int step, auto drafted) {
     constexpr bool DRAFT = decltype(drafted)::value;         // the step may have drafted keys
-    const uint32_t rows1 = row(step + 1, c1, p1);
-    auto ask = [&] {                      // for the pages of the step after next
-      c1 = c2;
-      p1 = page(step + 2, c1);
-      c2 = column(step + 3);
-    };
+    const uint32_t next = row(step + 1);
     if constexpr (WC > 1) {
       // the step has landed for every wave, and every wave is past the last one,
-      // whose place the next takes; the pages come after the transfers, since
-      // this wait is for all that was asked for before (tree_8x64x8200: 174 us
-      // with them before it, 157 so)
+      // whose place the next takes
       lds_ring_step<0>();
-      if (step + 1 < steps) issue(step + 1, rows1);
-      ask();
+      if (step + 1 < steps) issue(step + 1, next);
       __builtin_amdgcn_sched_barrier(0);
+    } else if (step + 1 < steps) {
+      issue(step + 1, next);
+      landed<2 * L::NTR>();
     } else {
-      // two steps' transfers on their way, for which the pages come first
-      ask();
-      if (step + 1 < steps) {
-        issue(step + 1, rows1);
-        landed<2 * L::NTR>();
-      } else {
-        landed<0>();
-      }
+      landed<0>();
     }
     uint4 *k = ring + (step & 1) * (2 * L::BYTES / 16), *v = k + L::BYTES / 16;
     const int key0 = key_of(step);
-    const unsigned long long ballot = __ballot(lane < TK && rows != kNoRow);
-    const Bits there = (Bits)ballot;                         // keys that some row may see
-    constexpr Bits kAll = (Bits)(~0ull >> (64 - TK));
+    const uint32_t there = (uint32_t)__ballot(lane < TK && rows != kNoRow);    // keys that some row may see
+    constexpr uint32_t kAll = ~0u >> (32 - TK);
     const bool trees = DRAFT && key0 + TK > sp.len;
-    Bits odd = 0;
+    uint32_t odd = 0;
     if (DRAFT) {
       // Drafted values that some rows see and others do not: 0 times an infinity
       // or NaN is not 0, so those leave the tile and go by themselves.  (The same
       // steps for all waves: they share tiles.)
       for (int e = lane; e < TK * L::CPR; e += 64)
-        if (C::odd_chunk(v[e])) odd |= (Bits)1 << (e / L::CPR);
+        if (C::odd_chunk(v[e])) odd |= (uint32_t)1 << (e / L::CPR);
 #pragma unroll
-      for (int s = 1; s < 64; s <<= 1) odd |= (Bits)__shfl_xor((long long)odd, s, 64);
+      for (int s = 1; s < 64; s <<= 1) odd |= (uint32_t)__shfl_xor((int)odd, s, 64);
       if constexpr (WC > 1) __syncthreads();
       if (odd != 0) {
         for (int e = lane; e < TK * L::CPR; e += 64) v[e] = C::even_chunk(v[e]);
@@ -596,7 +584,7 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
       pf_f32x4 sc[NB][NT];
       typename C::Values f;
       w.scores(k, v, f, sc);
-      Bits sees[NB];
+      uint32_t sees[NB];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) sees[nb] = there;
       if (trees) {
@@ -610,13 +598,13 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
           uint64_t x = at < a.words ? bits[at] >> sh : 0;
           if (sh > 0 && at + 1 < a.words) x |= bits[at + 1] << (64 - sh);
           if (d0 < 0) x = x << -d0 | ((1ull << -d0) - 1);    // (-d0 < TK)
-          sees[nb] &= (Bits)x;
+          sees[nb] &= (uint32_t)x;
         }
       }
       if (trees || there != kAll) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const Bits mine = sees[nb] >> (4 * grp);
+          const uint32_t mine = sees[nb] >> (4 * grp);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -664,8 +652,8 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
         }
       }
       w.outputs(v, f, sc, scale2, m, l);
-      for (Bits left = odd; left != 0; left &= left - 1) {
-        const int key = __builtin_amdgcn_readfirstlane(__builtin_ctzll(left));
+      for (uint32_t left = odd; left != 0; left &= left - 1) {
+        const int key = __builtin_amdgcn_readfirstlane(__builtin_ctz(left));
         const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)rows, key);
         const char *from = (const char *)a.v + (uint64_t)at * L::RB;
 #pragma unroll
@@ -690,7 +678,7 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
       }
     }
     wave_lds_sync();                      // the tile is read before anything takes its place
-    rows = rows1;
+    rows = next;
   };
   // (a loop without what only drafted keys need: with it the registers do not
   // suffice, and a spilled one's reload waits for the next tile's transfers)
@@ -840,10 +828,10 @@ SpanSizes sizes_of(int n, int draft, int n_heads, int n_kv_heads, int keys, bool
   // workgroups: 24 ragged trees of 25 take 100 us with 1024, 112 with 512, 158 with
   // 2048; 8 x 64 x 8200 179, 196 and 162; 32 rows of 4000 keys 131, 160 and 114.  At
   // most 4096 workgroups, 64 splits a sequence.
-  const int64_t least = std::min<int64_t>(1024, std::max<int64_t>(256, most * items / 512));
+  const int64_t least = std::min<int64_t>(1024, std::max<int64_t>(128, most * items / 512));
   z.least = std::max<int>(1, (int)(least / S::STEP));
   z.smax = (int)std::min<int64_t>(64, std::max<int64_t>(1, 4096 / items));
-  z.smax = (int)std::min<int64_t>(z.smax, std::max<int64_t>(1, (most + S::STEP - 1) / S::STEP / z.least));
+  z.smax = (int)std::min(z.smax, splits_of((int)((most + S::STEP - 1) / S::STEP), z.least));
   const size_t heads = (size_t)n * draft * n_heads;
   z.records = z.smax > 1 ? heads * z.smax * HD * sizeof(float) : 0;
   z.stats = z.smax > 1 || weigh ? heads * z.smax * sizeof(float2) : 0;
