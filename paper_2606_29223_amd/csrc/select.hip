@@ -129,6 +129,25 @@ __global__ __launch_bounds__(THREADS) void score_kernel(SelectArgs a, int stride
     page[e] = a.map.table[(size_t)x.seq * a.map.max_pages + min(c, x.columns - 1)];
     there[e] = c < x.columns && page[e] >= 0 && page[e] < a.map.n_pages;
   }
+  const T *src = (const T *)a.q + (int64_t)r * a.q_row + (int64_t)head * G * a.q_head + d * N;
+  auto query = [&](int g) {
+    const T *from = src + min(g, G - 1) * a.q_head;
+    Chunk<T> q;
+    if (whole) {
+      q.raw = *(const uint4 *)from;
+    } else {
+      T t[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) t[i] = from[i];
+      __builtin_memcpy(&q.raw, t, 16);
+    }
+    return q;
+  };
+  // (four heads' queries are asked for before the first is looked at)
+  constexpr int HEADS = 4;
+  Chunk<T> q[HEADS];
+#pragma unroll
+  for (int j = 0; j < HEADS; ++j) q[j] = query(j);
 #pragma unroll
   for (int e = 0; e < SCORE_EACH; ++e) {
     const T *b = (const T *)a.bounds + ((size_t)(there[e] ? page[e] : 0) * kv + head) * 2 * HD + d * N;
@@ -138,22 +157,20 @@ __global__ __launch_bounds__(THREADS) void score_kernel(SelectArgs a, int stride
   double up[N], down[N];                  // q+ and q-, of all the kv head's heads
 #pragma unroll
   for (int i = 0; i < N; ++i) up[i] = down[i] = 0.0;
-  const T *src = (const T *)a.q + (int64_t)r * a.q_row + (int64_t)head * G * a.q_head + d * N;
-  for (int g = 0; g < G; ++g, src += a.q_head) {
-    Chunk<T> q;
-    if (whole) {
-      q.raw = *(const uint4 *)src;
-    } else {
-      T t[N];
+  for (int g = 0; g < G; g += HEADS) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) t[i] = src[i];
-      __builtin_memcpy(&q.raw, t, 16);
+    for (int j = 0; j < HEADS; ++j) {
+      if (g + j >= G) break;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float v = q[j].get(i);
+        up[i] += v < 0.f ? 0.f : v;       // (a NaN goes on in both)
+        down[i] += v > 0.f ? 0.f : v;
+      }
     }
+    if (g + HEADS < G) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float v = q.get(i);
-      up[i] += v < 0.f ? 0.f : v;         // (a NaN goes on in both)
-      down[i] += v > 0.f ? 0.f : v;
+      for (int j = 0; j < HEADS; ++j) q[j] = query(g + HEADS + j);
     }
   }
   // a part of 0 adds nothing, whatever the bound (0 times infinity is not 0)

@@ -78,9 +78,8 @@ __global__ __launch_bounds__(kMaxDraft) void tree_accept_kernel(TreeAcceptArgs a
 // their rows' 16-byte chunks.  In place the entries go in turns: a turn's loads
 // are all done before its first store, and a source is never before its own
 // destination, so it is behind all earlier ones and no store overtakes a load.
-constexpr int KEEP_THREADS = 256, KEEP_EACH = 8;
-__global__ __launch_bounds__(KEEP_THREADS) void keep_kernel(KeepArgs a, int lanes, int slices, int pairs, int groups,
-                                                            int turns) {
+template <int THREADS, int EACH>
+__global__ __launch_bounds__(THREADS) void keep_kernel(KeepArgs a, int lanes, int slices, int pairs, int groups, int turns) {
   typedef __attribute__((ext_vector_type(4))) uint32_t chunk_t;
   const int kv = a.map.n_kv_heads;
   int x = blockIdx.x;
@@ -96,15 +95,15 @@ __global__ __launch_bounds__(KEEP_THREADS) void keep_kernel(KeepArgs a, int lane
   const size_t layer_rows = (size_t)a.map.n_pages * kv << a.map.shift;
   // entries of the pairs one after the other, `per` of them a turn (a list of more
   // than 256 has one pair)
-  const int per = KEEP_THREADS * KEEP_EACH / lanes, entries = n_pairs * n;
+  const int per = THREADS * EACH / lanes, entries = n_pairs * n;
   const int e_first = blockIdx.y * turns * per, e_end = min((int64_t)entries, (int64_t)e_first + (int64_t)turns * per);
   for (int e0 = e_first; e0 < e_end; e0 += per) {
-    chunk_t k[KEEP_EACH], v[KEEP_EACH];
-    size_t dst[KEEP_EACH];
-    bool go[KEEP_EACH];
+    chunk_t k[EACH], v[EACH];
+    size_t dst[EACH];
+    bool go[EACH];
 #pragma unroll
-    for (int e = 0; e < KEEP_EACH; ++e) {
-      const int item = e * KEEP_THREADS + threadIdx.x, in_turn = item / lanes, chunk = slice * lanes + item - in_turn * lanes;
+    for (int e = 0; e < EACH; ++e) {
+      const int item = e * THREADS + threadIdx.x, in_turn = item / lanes, chunk = slice * lanes + item - in_turn * lanes;
       const int entry = e0 + in_turn, in_pairs = pairs > 1 ? entry / n : 0, j = entry - in_pairs * n;
       const int pair = pair0 + in_pairs, layer = pair / kv, head = pair - layer * kv;
       go[e] = in_turn < per && entry < e_end && chunk * 16 < a.row_bytes;
@@ -128,7 +127,7 @@ __global__ __launch_bounds__(KEEP_THREADS) void keep_kernel(KeepArgs a, int lane
       __syncthreads();
     }
 #pragma unroll
-    for (int e = 0; e < KEEP_EACH; ++e)
+    for (int e = 0; e < EACH; ++e)
       if (go[e]) {
         *(chunk_t *)((char *)a.k + dst[e]) = k[e];
         *(chunk_t *)((char *)a.v + dst[e]) = v[e];
@@ -177,17 +176,28 @@ hipError_t launch_tree_accept(const TreeAcceptArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_keep(const KeepArgs &a, hipStream_t s) {
-  const int chunks = a.row_bytes / 16, all = a.n_layers * a.map.n_kv_heads;
-  // short lists (a tree's path) take several pairs a workgroup; long ones in place
-  // are slices of 128 bytes, so that more workgroups go through them in turns
-  const bool in_place = a.to == nullptr, brief = a.capacity <= 256;
-  const int lanes = !in_place || brief ? chunks : std::min(chunks, 8), slices = (chunks + lanes - 1) / lanes;
-  const int pairs = brief ? std::min(all, 8) : 1, groups = (all + pairs - 1) / pairs;
-  const int64_t blocks = (int64_t)a.map.n_seqs * groups * slices;
-  const int per = KEEP_THREADS * KEEP_EACH / lanes, most = (int)(((int64_t)pairs * a.capacity + per - 1) / per);
+  const int chunks = a.row_bytes / 16;
+  const int64_t all = (int64_t)a.n_layers * a.map.n_kv_heads, rows = all * a.map.n_seqs;
+  // Short lists (a tree's path) take several pairs a workgroup, as long as there
+  // are 512 workgroups: 4 lists of 200 in 8 heads 67 us with eight pairs, 10 with
+  // one.  Long ones in place go in turns of as much as 1024 threads hold, in slices
+  // of 128 bytes, or of 64 where those are fewer than 256 workgroups: 128 lists of
+  // 2000 of bf16 rows of 128 53 us (4.9 TB/s; 76 with the narrow ones), 16 of 4000
+  // 32 (51 with the wide ones).  What does not wait for itself has few loads a
+  // thread and many workgroups: 192 lists of up to 1999 fp32 rows of 64 into new
+  // pages 70 us with two of 16 bytes, 79 with eight.
+  const bool in_place = a.to == nullptr, brief = a.capacity <= 256, turn = in_place && !brief;
+  const int wide = std::min(chunks, 8), narrow = std::min(chunks, 4);
+  const int lanes = !turn ? chunks : rows * ((chunks + wide - 1) / wide) >= 256 ? wide : narrow;
+  const int slices = (chunks + lanes - 1) / lanes;
+  const int pairs = brief ? (int)std::max<int64_t>(1, std::min<int64_t>(8, rows / 512)) : 1;
+  const int64_t groups = (all + pairs - 1) / pairs, blocks = (int64_t)a.map.n_seqs * groups * slices;
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  const int per = (turn ? 1024 * 4 : 512 * 2) / lanes, most = (int)(((int64_t)pairs * a.capacity + per - 1) / per);
   const int split = in_place ? 1 : std::min(most, 65535), turns = (most + split - 1) / split;
-  keep_kernel<<<dim3((unsigned)blocks, split), KEEP_THREADS, 0, s>>>(a, lanes, slices, pairs, groups, turns);
+  const dim3 grid((unsigned)blocks, split);
+  if (turn) keep_kernel<1024, 4><<<grid, 1024, 0, s>>>(a, lanes, slices, pairs, (int)groups, turns);
+  else keep_kernel<512, 2><<<grid, 512, 0, s>>>(a, lanes, slices, pairs, (int)groups, turns);
   return hipGetLastError();
 }
 
