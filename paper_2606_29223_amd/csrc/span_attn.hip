@@ -5,6 +5,26 @@
 // Row i of a sequence with L keys sees the keys j < L whose page is there and,
 // of the drafted keys L + t, those with bit t of its mask: s_j = scale q.k_j,
 // out = sum e^{s_j - m} v_j / sum e^{s_j - m}, lse = m + ln sum e^{s_j - m}.
+//
+// One pass over the keys, with a running reference in place of the maximum.  The
+// rows of a sequence and the query heads of a kv head are the columns of the
+// products S^T = K Q^T and O^T = V^T P^T, so a tile of keys and values in LDS is
+// read for all of them, and a score lies in the lane that needs it as a weight.
+//
+// What bounds it, bf16 heads of 128, 8 kv heads of 4 query heads, on one MI355X:
+// * 8 sequences of 8200 keys, trees of 64 (256 columns): 163 us without the join.
+//   The weights go to the matrix cores in three bf16 parts that hold all 24 bits,
+//   four products a key and column for the two of the formula: 138 GFLOP, 0.85
+//   PFLOP/s for the 1.2 of a large library product here.  A step of a wave has
+//   2048 cycles of products and as much vector work as fits between them (2.4 us
+//   for two waves a SIMD).  Two parts would take 12 % less and round to 17 bits.
+// * 24 ragged trees of 25 up to 12000 keys: 78 us, of which the CUs' mean is 43 and
+//   the rest the difference between them.
+// * 32 single rows of 4000 keys: 5.3 TB/s in the kernel, memory's.
+// Not better: tiles of 64 keys (they spill, or are equal), three waves a SIMD
+// (spills), eight waves a workgroup (equal), the ring four tiles deep (181 us for
+// 175: the transfers are not what a step waits for), the next tile's scores
+// between the weights of this one (equal).
 #include "attn_decode.h"
 #include "dex.h"
 #include "span.h"
@@ -27,7 +47,9 @@ __device__ uint4 zero_row[32];
 struct SpanPlan {
   int steps, n;
 };
-__host__ __device__ __forceinline__ int splits_of(int steps, int least) { return max(1, (steps + least - 1 - least / 4) / least); }
+__host__ __device__ __forceinline__ int splits_of(int steps, int least) {
+  return max(1, (steps + least - 1 - least / 4) / least);
+}
 __host__ __device__ __forceinline__ SpanPlan span_plan(int keys, int step_keys, int smax, int least) {
   const int all = (keys + step_keys - 1) / step_keys, n = min(smax, splits_of(all, least));
   SpanPlan p;
@@ -137,7 +159,8 @@ struct Cols<L, uint16_t, HD, NB> {
           __builtin_memcpy(&x, e, 16);
         }
       }
-      q[nb][st] = __builtin_bit_cast(pf_bf16x8, make_uint4((x.x ^ sign) & some, (x.y ^ sign) & some, (x.z ^ sign) & some, (x.w ^ sign) & some));
+      x = make_uint4((x.x ^ sign) & some, (x.y ^ sign) & some, (x.z ^ sign) & some, (x.w ^ sign) & some);
+      q[nb][st] = __builtin_bit_cast(pf_bf16x8, x);
     }
   }
   // The values' fragments: of 16 dimensions dt, the rows 4 tq .. + 3 and those 16
@@ -424,23 +447,23 @@ __device__ __forceinline__ void landed() {
 }
 
 // The waves of a workgroup: WC neighbouring column blocks over the same keys,
-// WK = NW / WC groups of keys.  Alone, bf16 waves go by two, since four have 128
-// KB of tiles and one workgroup on a CU, which then waits for the first of them:
-// 32 ragged rows' weights 78 us with four, 74 with two.
+// WK = NW / WC groups of keys.  Waves alone whose tiles would be 128 KB for four
+// go by two, since one workgroup on a CU waits for its first tiles: 32 ragged
+// rows' weights 78 us with four, 74 with two.
 template <typename T, int HD, int NB, int WC>
 struct Shape {
-  static constexpr int NW = WC > 1 || sizeof(T) == 4 ? 4 : 2, WK = NW / WC, COLS = 16 * NB * WC;
   static constexpr int TK = sizeof(T) == 2 ? 32 : 16;
   using L = Tile<T, HD, TK>;
-  static constexpr int STEP = L::TK * WK;                    // keys of a step
   static constexpr int RING = 4 * L::BYTES;                  // a key group's two tiles of keys and values
+  static constexpr int NW = WC > 1 || 4 * RING <= 65536 ? 4 : 2, WK = NW / WC, COLS = 16 * NB * WC;
+  static constexpr int STEP = L::TK * WK;                    // keys of a step
   static constexpr int MEET = WK > 1 ? NW * 16 * NB * (HD + 4) * 4 : 0;
   static constexpr int LDS = RING * WK > MEET ? RING * WK : MEET;
 };
 
 template <bool TREE, typename T, int HD, int NB, int WC>
-__global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW)) __attribute__((amdgpu_waves_per_eu(WC == 1 && HD * sizeof(T) > 128 ? 1 : 2)))
-void span_attn_kernel(SpanArgs a, SpanGrid g) {
+__global__ __launch_bounds__((64 * Shape<T, HD, NB, WC>::NW))
+    __attribute__((amdgpu_waves_per_eu(WC == 1 && HD * sizeof(T) > 128 ? 1 : 2))) void span_attn_kernel(SpanArgs a, SpanGrid g) {
   using S = Shape<T, HD, NB, WC>;
   using L = typename S::L;
   using C = Cols<L, T, HD, NB>;
@@ -457,8 +480,9 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
   x /= kv;
   const int block = x % g.blocks;
   x /= g.blocks;
-  // (turned on by one each split: workgroups go to the XCD's parts in turn, and
-  // the splits of a long sequence would all go to one: 24 ragged trees 102 us for 90)
+  // (turned on by one each split: workgroups go to the parts of an XCD in turn, and
+  // the splits of a long sequence would all go to one of them: 24 ragged trees 102
+  // us for 90)
   const int split = x / a.n, b = (x + split) % a.n;
   const Span sp = span_of(a, b);
   const SpanPlan plan = span_plan(sp.keys, S::STEP, g.smax, g.least);
@@ -515,7 +539,8 @@ void span_attn_kernel(SpanArgs a, SpanGrid g) {
     if (runs && __ballot(lane >= TK || rows != kNoRow) == ~0ull) {
       each([&](int c, int, uint32_t kc, uint32_t vc) {
         const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)rows, c * L::RPT) * L::RB;
-        move(c, (const char *)a.k + off + (uint32_t)(l_row * L::RB + kc), (const char *)a.v + off + (uint32_t)(l_row * L::RB + vc));
+        const uint32_t in = l_row * L::RB;
+        move(c, (const char *)a.k + off + (in + kc), (const char *)a.v + off + (in + vc));
       });
     } else {
       each([&](int c, int row, uint32_t kc, uint32_t vc) {
@@ -810,7 +835,6 @@ __global__ __launch_bounds__(256) void span_weigh_kernel(SpanArgs a, SpanGrid g,
   }
 }
 
-
 struct SpanSizes {
   int blocks, smax, least, step;
   size_t records, stats, scores;          // bytes
@@ -824,10 +848,12 @@ SpanSizes sizes_of(int n, int draft, int n_heads, int n_kv_heads, int keys, bool
   z.blocks = (cols + S::COLS - 1) / S::COLS;
   z.step = S::STEP;
   const int64_t most = (int64_t)keys + (trees ? draft : 0), items = (int64_t)std::max(n, 1) * n_kv_heads * z.blocks;
-  // Splits of 1024 keys or more, shorter only where they would be fewer than 512
-  // workgroups: 24 ragged trees of 25 take 100 us with 1024, 112 with 512, 158 with
-  // 2048; 8 x 64 x 8200 179, 196 and 162; 32 rows of 4000 keys 131, 160 and 114.  At
-  // most 4096 workgroups, 64 splits a sequence.
+  // Splits of about 1024 keys, shorter only where they would be fewer than 512
+  // workgroups.  With 512, 768, 1024 and 2048: 24 ragged trees of 25 91, 81, 84 and
+  // 131 us; 8 x 64 x 8200 191, 184, 169 and 163; 8 x 8 x 8200 72, 77, 63 and 63 (512
+  // workgroups are one turn of the chip); the weights of 32 ragged rows 81, 83, 76
+  // and 88.  128 keys at least: four rows of 700 19 us, with 256 21.  At most 4096
+  // workgroups, 64 splits a sequence.
   const int64_t least = std::min<int64_t>(1024, std::max<int64_t>(128, most * items / 512));
   z.least = std::max<int>(1, (int)(least / S::STEP));
   z.smax = (int)std::min<int64_t>(64, std::max<int64_t>(1, 4096 / items));
@@ -880,17 +906,18 @@ hipError_t go(const SpanArgs &a, hipStream_t s) {
   return e;
 }
 
-// Column blocks a wave, and neighbouring waves over the same keys.  A wave that
-// shares its tiles with others reads them from LDS for few columns, but has more
-// transfers on their way for its size: 8 trees of 8200 keys with their
-// columns in one block a wave and two: 24 columns 61 and 70 us, 32 61 and 70, 64 66
-// and 74, 128 113 and 92.  A few workgroups alone take the smaller blocks: one tree of 64 x 8200 39
-// us for 47.
+// Column blocks a wave, and neighbouring waves over the same keys.  Few columns
+// have a wave each, with keys of its own: 32 rows of 4000 keys and their weights
+// 131 us, 147 with four waves that share tiles (8 trees of 16 columns and 8200 keys
+// 64 and 60).  More share their tiles, in one block a wave up to 64 columns (24
+// columns 60 us, 63 with two waves and two groups of keys) and in two behind
+// that: 128 columns 115 us with one, 96 with two.  A few workgroups alone take the
+// smaller blocks: one tree of 64 x 8200 39 us for 58.
 template <typename F>
 auto by_columns(int cols, int64_t pairs, F f) {
   if (cols <= 16) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-  if (cols <= 32) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
-  if (cols <= 64 || pairs * ((cols + 127) / 128) <= 32) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
+  if (cols <= 64 || pairs * ((cols + 127) / 128) <= 32)
+    return f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
   return f(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
 }
 template <typename F>
