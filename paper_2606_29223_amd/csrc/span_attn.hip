@@ -805,34 +805,64 @@ __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, SpanGrid g, 
   finish<T>(a, g.whole, row, head, d, o, m, l);
 }
 
-// The weights of a row's keys, from its scores and sums, added to its totals.
-__global__ __launch_bounds__(256) void span_weigh_kernel(SpanArgs a, SpanGrid g, int step_keys, int chunk, int parts) {
+// The reference and the sum of a row's n splits, eight of them asked for at once.
+__device__ __forceinline__ float2 stats_of(const float2 *stat, int n) {
+  auto each = [&](auto f) {
+    for (int s0 = 0; s0 < n; s0 += 8) {
+      float2 st[8];
+#pragma unroll
+      for (int s = 0; s < 8; ++s) st[s] = stat[min(s0 + s, n - 1)];
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        if (s0 + s < n) f(st[s]);
+    }
+  };
+  float m = -INFINITY, l = 0.f;
+  each([&](float2 st) { m = fmaxf(m, st.x); });
+  const float ref = m == -INFINITY ? 0.f : m;
+  each([&](float2 st) { l = fmaf(__builtin_amdgcn_exp2f(st.x - ref), st.y, l); });
+  return make_float2(m, l);
+}
+
+// The weights of a row's keys, from its scores and sums, added to its totals.  A
+// lane has four neighbouring keys, whose loads are all on their way at once: the
+// kernel is the latency of lengths, sums and scores, one after the other.
+constexpr int WEIGH_KEYS = 4 * 256;
+__global__ __launch_bounds__(256) void span_weigh_kernel(SpanArgs a, SpanGrid g, int step_keys, int parts) {
   __shared__ float2 norm[64];             // of a query head: reference, 1 / sum
   const int kv = a.map.n_kv_heads, G = a.n_heads / kv;
-  const int id = blockIdx.x / parts, head = id % kv, b = id / kv, first = (blockIdx.x - id * parts) * chunk;
+  const int id = blockIdx.x / parts, head = id % kv, b = id / kv, first = (blockIdx.x - id * parts) * WEIGH_KEYS;
   const Span sp = span_of(a, b);
   if (first >= sp.len) return;
-  const int n = span_plan(sp.keys, step_keys, g.smax, g.least).n;
-  for (int h = threadIdx.x; h < G; h += 256) {
-    const size_t base = rec_index(a, b, head * G + h, 0, g.smax);
-    float m = -INFINITY, l = 0.f;
-    for (int s = 0; s < n; ++s) m = fmaxf(m, g.stat[base + s].x);
-    const float ref = m == -INFINITY ? 0.f : m;
-    for (int s = 0; s < n; ++s) l = fmaf(__builtin_amdgcn_exp2f(g.stat[base + s].x - ref), g.stat[base + s].y, l);
-    norm[h] = make_float2(ref, inverse(l));
-  }
-  __syncthreads();
   const size_t row = (size_t)b * kv + head;
   const float *in = a.weight + row * a.weight_ld;
   float *out = a.weight_out + row * a.weight_out_ld;
   const float *score = g.score + ((size_t)b * a.n_heads + head * G) * g.score_ld;
-  for (int j = first + threadIdx.x; j < min(first + chunk, sp.len); j += 256) {
-    float sum = 0.f;
-    if (page_row(a.map, sp.seq, j, head) != kNoRow) {
-      for (int h = 0; h < G; ++h) sum += __builtin_amdgcn_exp2f(score[(size_t)h * g.score_ld + j] - norm[h].x) * norm[h].y;
-    }
-    out[j] = in[j] + sum;
+  const int j0 = first + 4 * threadIdx.x, last = sp.len - 1;
+  float total[4];
+  bool there[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    total[i] = in[min(j0 + i, last)];
+    there[i] = page_row(a.map, sp.seq, min(j0 + i, last), head) != kNoRow;
   }
+  if (threadIdx.x < G) {
+    const int n = span_plan(sp.keys, step_keys, g.smax, g.least).n;
+    const float2 all = stats_of(g.stat + rec_index(a, b, head * G + threadIdx.x, 0, g.smax), n);
+    norm[threadIdx.x] = make_float2(all.x == -INFINITY ? 0.f : all.x, inverse(all.y));
+  }
+  __syncthreads();
+  if (j0 > last) return;
+  pf_f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int h = 0; h < G; ++h) {
+    const pf_f32x4 x = *(const pf_f32x4 *)(score + (size_t)h * g.score_ld + j0);     // (rows of whole steps)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(x[i] - norm[h].x) * norm[h].y;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (j0 + i <= last) out[j0 + i] = total[i] + (there[i] ? sum[i] : 0.f);
 }
 
 struct SpanSizes {
@@ -897,10 +927,9 @@ hipError_t go(const SpanArgs &a, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   if (weigh && a.max_len > 0) {
-    const int chunk = 1024;
-    const int64_t parts = ((int64_t)a.max_len + chunk - 1) / chunk, blocks = parts * a.n * a.map.n_kv_heads;
+    const int64_t parts = ((int64_t)a.max_len + WEIGH_KEYS - 1) / WEIGH_KEYS, blocks = parts * a.n * a.map.n_kv_heads;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    span_weigh_kernel<<<(unsigned)blocks, 256, 0, s>>>(a, g, z.step, chunk, (int)parts);
+    span_weigh_kernel<<<(unsigned)blocks, 256, 0, s>>>(a, g, z.step, (int)parts);
     e = hipGetLastError();
   }
   return e;
