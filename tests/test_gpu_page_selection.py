@@ -196,3 +196,18 @@ def test_strided_queries_and_outputs():
     assert all(np.array_equal(a, host(b)) for a, b in zip(want, got))
     y[:, 2:8, 3:67] = 9.0
     assert (y == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd,page", [(64, 1), (128, 2), (32, 4)])
+def test_lists_of_more_columns_than_a_wave_holds(dtype, hd, page):
+    """Lists on both sides of 64 columns, in any order, some of them twice or none
+    of the table's, some of their pages missing."""
+    torch_cuda()
+    n = 300
+    c = Case(hd, dtype, hd, 8, 2, page, [61 * page, 64 * page, 65 * page + 1, 300 * page, 40 * page - 1, 0])
+    columns = c.rng.integers(-2, 310, (6, 2, n))
+    t = c.table.copy()
+    t[3, 5::7] = -1
+    columns = ints(columns)
+    c.check(c.attend(columns, table=t), columns, table=t)

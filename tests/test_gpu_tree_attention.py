@@ -77,6 +77,59 @@ def test_long_sequences(dtype, hd, draft):
     c.check(c.run())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd,draft", [(128, 3), (64, 13), (128, 30)])
+@pytest.mark.parametrize("page", [1, 2])
+def test_more_pages_than_a_wave_holds(dtype, hd, draft, page):
+    """64 columns of a table are looked at at once: keys on both sides of that, and
+    of the splits, some of their pages missing."""
+    torch_cuda()
+    c = Case(hd + page, dtype, hd, 8, 2, page, [0, 61, 63, 64, 65, 127, 129, 703, 2000], draft)
+    t = c.table.copy()
+    t[3:, 5::7] = -1
+    c.check(c.run(table=t), table=t)
+
+
+def many_wide(dtype, hd, page):
+    """Trees of 20 with four heads a kv head, 80 columns, in enough (tree, kv head)
+    pairs that a wave takes two blocks of columns."""
+    lens = [0, 1, 30, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129, 255, 257, 300, 511, 1500, 3100, 12]
+    return Case(hd + page, dtype, hd, 8, 2, page, lens, 20, drafts=[20, 1, 0, 19] * 4 + [20, 20, 7, 20])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd,page", [(32, 4), (64, 1), (64, 16), (128, 2), (128, 64)])
+def test_many_wide_trees(dtype, hd, page):
+    torch_cuda()
+    c = many_wide(dtype, hd, page)
+    c.check(c.run())
+    t = c.table.copy()
+    t[10:, 3::5] = -1
+    c.check(c.run(table=t), table=t)
+    seq = np.array([19, 18, 17, -1, 20] + list(range(15)))
+    lens = np.concatenate((c.lens[19:16:-1], [40, 40], c.lens[:15]))
+    drafts = np.concatenate((c.drafts[19:16:-1], [20, 20], c.drafts[:15]))
+    c.check(c.run(seq=ints(seq), lens=lens, drafts=drafts), seq=seq, lens=lens, drafts=drafts)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_wide_trees_with_values_that_only_some_rows_see(dtype):
+    torch_cuda()
+    c = many_wide(dtype, 64, 16)
+    c.seen[:] = np.eye(20, dtype=bool)
+    c.seen[:, 10:, 1] = True
+    clean = [host(t) for t in c.run()]
+    sees = np.zeros((20, 20), bool)
+    for b, n in enumerate(c.lens):
+        if c.drafts[b] > 1:
+            c.v[int(c.table[b, (n + 1) // 16]), :, (n + 1) % 16, 7] = float("-inf")
+            sees[b] = c.seen[b, :, 1] & (np.arange(20) < c.drafts[b])
+    got = [host(t) for t in c.run()]
+    sees = sees.reshape(-1)
+    assert np.isneginf(got[0][sees][..., 7]).all() and np.array_equal(got[0][~sees], clean[0][~sees])
+    assert np.array_equal(np.delete(got[0], 7, 2), np.delete(clean[0], 7, 2)) and np.array_equal(got[1], clean[1])
+
+
 def test_drafts_out_of_range_and_sequences_that_are_none():
     """Rows from n_draft on get zeros and -inf; n_draft, lens and sequences out
     of range are clamped or leave the tree empty."""
