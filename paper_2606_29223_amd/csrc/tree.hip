@@ -3,7 +3,7 @@
 //
 // But for the moved rows these are a few hundred integers and bounded by the
 // latency of a launch and of their loads one after the other: 16 trees of 64,
-// masks 2.5 us, paths 3.9, rows of 32 layers x 8 heads 6.2 (4.7 MB read and written),
+// masks 2.5 us, paths 3.4, rows of 32 layers x 8 heads 6.2 (4.7 MB read and written),
 // pages 5.2.  Moved rows of a long list are a copy, bounded by memory: 192 lists of up
 // to 1999 fp32 rows of 64 into new pages 70 us, 300 MB, 4.3 TB/s.
 #include "dex.h"
@@ -45,38 +45,42 @@ __global__ __launch_bounds__(kMaxDraft) void tree_mask_kernel(TreeMaskArgs a) {
 }
 
 // A lane a node walks to its root and sees whether every token on the way is
-// the one wanted; the deepest such node wins, the lowest number among equals.
+// the one wanted; the deepest such node wins, the lowest number among equals.  A
+// node's own token is looked at first, so that a step of the way is one LDS read:
+// 256 nodes 2.8 us as a binary tree, 30 as one chain that is accepted.
 __global__ __launch_bounds__(kMaxDraft) void tree_accept_kernel(TreeAcceptArgs a) {
-  __shared__ int parent[kMaxDraft], token[kMaxDraft], target[kMaxDraft], path[kMaxDraft], best;
+  constexpr int kUnwanted = -2;
+  __shared__ int up[kMaxDraft], target[kMaxDraft], path[kMaxDraft], best;
   const int i = threadIdx.x, b = blockIdx.x;
   const size_t at = (size_t)b * a.draft + i;
   const int n = a.n_draft != nullptr ? max(0, min(a.n_draft[b], a.draft)) : a.draft;
-  if (i < n) {
-    parent[i] = parent_of(a.parent[at], i);
-    token[i] = a.token[at];
+  const int root = a.root != nullptr ? a.root[b] : -1;
+  int parent = -1, token = 0;
+  if (i < a.draft) {
+    parent = parent_of(a.parent[at], i);
+    token = a.token[at];
     target[i] = a.target[at];
   }
   path[i] = -1;
   if (i == 0) best = 0;
   __syncthreads();
-  if (i < n) {
-    int depth = 0;
-    bool ok = true;
-    for (int j = i; j >= 0 && ok; j = parent[j]) {
-      ++depth;
-      const int p = parent[j];
-      ok = p >= 0 ? token[j] == target[p] : a.root == nullptr || token[j] == a.root[b];
-    }
-    if (ok) atomicMax(&best, depth << 16 | (0xffff - i));
+  // its parent, if its token is the one wanted
+  const bool own = i < n && (parent >= 0 ? token == target[parent] : a.root == nullptr || token == root);
+  up[i] = own ? parent : kUnwanted;
+  __syncthreads();
+  if (own) {
+    int depth = 1, j = parent;
+    for (; j >= 0; j = up[j]) ++depth;
+    if (j != kUnwanted) atomicMax(&best, depth << 16 | (0xffff - i));
   }
   __syncthreads();
   const int depth = best >> 16, last = 0xffff - (best & 0xffff);
   if (i == 0) {
     int at_depth = depth;
     if (depth > 0)
-      for (int j = last; j >= 0; j = parent[j]) path[--at_depth] = j;
+      for (int j = last; j >= 0; j = up[j]) path[--at_depth] = j;
     a.count[b] = depth;
-    a.next[b] = depth > 0 ? target[last] : a.root != nullptr ? a.root[b] : -1;
+    a.next[b] = depth > 0 ? target[last] : root;
   }
   __syncthreads();
   if (i < a.draft) a.path[at] = path[i];
