@@ -580,9 +580,12 @@ dex_status dex_tree_accept(const int32_t *parent, const int32_t *token, const in
  * its rotary position is tree_len[b] + depth, so turn it with dex_rope first).
  * The row sees the keys before the tree, and node j's if bit j of mask[b][i] is
  * set, j < tree_draft[b] (NULL: draft), each only where its page is there; the
- * mask may be any, and what it hides has no effect, NaN and infinity neither.
- * Softmax, out and lse as dex_pages_attention's; a row that sees nothing, and
- * the rows from tree_draft[b] on, get zeros and -inf.                         */
+ * mask may be any, and what it hides has no effect: large values, NaN and
+ * infinity neither.  Softmax, out and lse as dex_pages_attention's, in all
+ * attention below: a weight under 2^-126 of the row's largest may count as 0 (in
+ * bf16 as 2^-132), and an infinite value with such a weight gives infinity or
+ * NaN.  A row that sees nothing, and the rows from tree_draft[b] on, get zeros
+ * and -inf.                                                                   */
 int64_t dex_pages_tree_attention_work(int32_t dtype, int32_t n_trees, int32_t draft, int32_t n_heads, int32_t n_kv_heads,
                                       int32_t head_dim, int32_t max_len);
 dex_status dex_pages_tree_attention(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads, int32_t n_trees,
