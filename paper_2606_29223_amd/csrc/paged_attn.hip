@@ -144,13 +144,15 @@ __device__ __forceinline__ const char *row_at(const void *base, uint32_t rows, i
 
 // A float's upper half is a bf16, and what is left of its 24 bits after that two
 // more: three parts that are the float, with no rounding.  Where nothing is left
-// a part is 2^-100, not 0, so that an infinite value times its weight, the sum
-// over the parts, is infinite (0 and negative parts would make it NaN).
+// a part is the least bf16, 2^-133 (the products keep it), not 0, so that an
+// infinite value times its weight, the sum over the parts, is infinite (0 would
+// make it NaN).  The two add at most 2^-132 to a weight, which goes to 0 below
+// 2^-126 in the power already.
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 __device__ __forceinline__ float after_upper(float a) {
-  return fmaxf(a - __uint_as_float(__float_as_uint(a) & 0xffff0000u), 0x1p-100f);
+  return fmaxf(a - __uint_as_float(__float_as_uint(a) & 0xffff0000u), 0x1p-133f);
 }
 
 // bf16: a tile is a unit.  Keys and values come as whole rows, 1 KB a load

@@ -117,3 +117,28 @@ def test_small_weights_of_large_and_infinite_values(dtype, score):
     for bad in (float("inf"), float("-inf")):
         for got in _every_form(*_underflow(dtype, keys, at, score, bad), keys):
             assert (got[..., 3] == bad).all() and np.isfinite(np.delete(got, 3, 2)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 4])
+def test_large_values_of_single_rows(dtype, group):
+    """The same for attention of one token a row, alone and in a group whose
+    pages are read once: weights of 0 in float, and small ones of large and
+    infinite values."""
+    torch_cuda()
+    from paper_2606_29223_amd import paged
+    keys, at = 900, 500
+    run = lambda q, k, v, table: host(paged.attention(q.expand(4, -1, -1).contiguous(), k, v, table.expand(4, -1).contiguous(),
+                                                      ints([keys] * 4), scale=1.0, group=group))
+    for big in LARGE:
+        tol = (2 * (keys + 128) + 8) * 2.0 ** -24 + HALF_STEP[dtype] + (2.0 ** -132 * abs(big) / keys if dtype == "bf16" else 0)
+        assert np.abs(run(*_underflow(dtype, keys, at, -1000.0, big)) - 1.0).max() <= tol, big
+    for score in (-40.0, -84.0):
+        value, p = float(torch_cuda().tensor(2.0 * np.exp(-score)).bfloat16()), np.exp(score)
+        want = (keys - 1 + p * value) / (keys - 1 + p)
+        rel = 2.0 ** -22 + 123 * 2.0 ** -24 + 2.0 ** -132 / p + 2 * (keys + 128) * 2.0 ** -24
+        got = run(*_underflow(dtype, keys, at, score, value))
+        assert np.abs(got[..., 3] - want).max() <= rel * want + HALF_STEP[dtype] * 1.01 * want
+        for bad in (float("inf"), float("-inf")):
+            got = run(*_underflow(dtype, keys, at, score, bad))
+            assert (got[..., 3] == bad).all() and np.isfinite(np.delete(got, 3, 2)).all()
