@@ -577,7 +577,9 @@ dex_status dex_tree_accept(const int32_t *parent, const int32_t *token, const in
  * node i of tree b, of sequence tree_seq[b] (NULL: b) with tree_len[b] keys
  * before the tree (a longer one counts as max_len, below 0 as 0); node j's key
  * and value are at position tree_len[b] + j (dex_pages_append puts them there;
- * its rotary position is tree_len[b] + depth, so turn it with dex_rope first).
+ * its rotary position is tree_len[b] + depth, so turn it with dex_rope first;
+ * where dex_pages_reserve granted nothing, pos -1, every row_pos of the tree is
+ * -1 and its tree_draft 0).
  * The row sees the keys before the tree, and node j's if bit j of mask[b][i] is
  * set, j < tree_draft[b] (NULL: draft), each only where its page is there; the
  * mask may be any, and what it hides has no effect: large values, NaN and

@@ -27,19 +27,23 @@ A step of a decoding loop with branches, for a model of the caller's:
     parent, token, score, done = paged.beam_select(logits, score, done=done, eos=eos)
     cache.fork(parent.flatten())                      # the branches follow their parents
 
-A step with drafted tokens, `draft` of them a sequence in trees:
+A step with drafted tokens, up to `draft` of them a sequence in trees (a
+sequence that reserve grants nothing, asked for or not, stays as it is):
 
     mask, depth = paged.tree_mask(parent)
     before = cache.lens.clone()
-    pos = cache.reserve(n_draft).pos                   # n_draft: draft for every sequence
+    place = cache.reserve(n_draft).places(draft).flatten()   # n_draft: each tree's tokens, 0 to draft
+    granted = cache.lens - before                      # n_draft, or 0
     at = (before[:, None] + depth).flatten()           # rotary positions
-    place = (pos[:, None] + torch.arange(draft, dtype=torch.int32, device=pos.device)).flatten()
     for layer in range(cache.n_layers):
         q, k = paged.rope(rotary, at, q, k)
         cache.append(layer, place, q, k, v, seq=seq)   # seq: each row's sequence
-        out = cache.tree_attention(layer, q, before, mask)
-    path, count, token = paged.tree_accept(parent, drafted, target)
+        out = cache.tree_attention(layer, q, before, mask, n_draft=granted)
+    path, count, token = paged.tree_accept(parent, drafted, target, n_draft=granted, root=token)
     cache.accept(before, path, count)                  # the path's tokens stay, the others go
+
+Here every tree's first node is its sequence's last token, `token`, which stays
+the next one where nothing was granted.
 """
 
 from __future__ import annotations
@@ -318,6 +322,12 @@ class Reserved(NamedTuple):
     dst: torch.Tensor
     tokens: torch.Tensor
     state: torch.Tensor
+
+    def places(self, draft):
+        """The positions [n_seqs, draft] of each sequence's `draft` tokens from pos
+        on, as `append` takes them: all -1 where nothing was granted."""
+        pos = self.pos[:, None]
+        return torch.where(pos < 0, -1, pos + torch.arange(draft, dtype=torch.int32, device=pos.device))
 
 
 def reserve(table, ref, lens, n_new, page_size):
@@ -794,8 +804,12 @@ class PagedCache:
         return tree_attention(q, self.k[layer], self.v[layer], self.table, lens, mask, **kw)
 
     def accept(self, lens, path, count):
-        """Of the tokens from lens [n_seqs] on, those of the path (`tree_accept`)
-        stay, behind the sequence; the rest and their pages are given back."""
+        """Of the tokens that each sequence holds from lens [n_seqs] on (its length
+        before `reserve`), those of the path stay, behind the sequence; the rest and
+        their pages are given back.  path and count as `tree_accept` gives them for
+        the trees' tokens that were granted (n_draft); a sequence without any stays
+        as it is."""
+        count = torch.minimum(count, self.lens - lens)
         keep(self.k, self.v, self.table, path, count, first=lens)
         torch.add(lens, count, out=self.lens)
         trim(self.table, self.ref, self.lens, self.page_size)
