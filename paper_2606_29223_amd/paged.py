@@ -841,6 +841,8 @@ class PagedCache:
         that they have, and new tokens need positions of the caller's own count."""
         if weight.dim() != 4 or weight.shape[:3] != (self.n_layers, len(self.lens), self.k.shape[2]):
             _refuse("weight is [n_layers, n_seqs, n_kv_heads, n]")
+        if not weight.is_contiguous():            # (flattened it would be a copy, and only that be cut)
+            _refuse("weight is not contiguous")
         self._check_copy()
         n = len(self.lens)
         index, count = evict(weight.flatten(0, 1), self.lens.repeat(self.n_layers), budget, sinks=sinks, recent=recent)

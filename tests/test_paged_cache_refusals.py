@@ -1,0 +1,28 @@
+"""PagedCache refuses calls whose results would not be the caller's tensors or the
+caller's rows, before anything is launched."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2606_29223_amd import dexlib, paged  # noqa: E402
+
+LAYERS, KV, HD, PS, SEQS, WIDTH = 2, 2, 32, 4, 3, 5
+
+
+def cache(**kw):
+    return paged.PagedCache(LAYERS, KV, HD, PS, 8, SEQS, WIDTH, device="cpu", **kw)
+
+
+@pytest.mark.parametrize("view", [
+    lambda n: torch.zeros((SEQS, LAYERS, KV, n)).transpose(0, 1),
+    lambda n: torch.zeros((LAYERS, SEQS, n, KV)).transpose(2, 3),
+    lambda n: torch.zeros((LAYERS, SEQS, KV, n + 4))[..., :n],
+    lambda n: torch.zeros((LAYERS, SEQS + 1, KV, n))[:, 1:],
+    lambda n: torch.zeros((LAYERS, 1, KV, n)).expand(LAYERS, SEQS, KV, n)])
+def test_evict_refuses_weights_that_it_could_not_cut_in_place(view):
+    """Flattened over layers and sequences these are copies: the caller's totals
+    would stay as they were."""
+    weight = view(PS * WIDTH)
+    assert weight.shape == (LAYERS, SEQS, KV, PS * WIDTH)
+    with pytest.raises(dexlib.DexError, match="contiguous"):
+        cache().evict(weight, 4)
