@@ -822,17 +822,29 @@ class PagedCache:
             _refuse("the cache keeps no bounds (bounds=True)")
         page_bounds(self.k[layer], self.table, self.lens, n_new=n_new, out=self.bounds[layer])
 
-    def sparse_attention(self, layer, q, n_select, sinks=1, recent=1, **kw):
+    def _row_lens(self, lens, seq):
+        """The rows' lengths: by default row r is sequence r, over all its tokens."""
+        if lens is None and seq is not None:
+            _refuse("rows of other sequences (seq) go with their lengths (lens)")
+        return self.lens if lens is None else lens
+
+    def sparse_attention(self, layer, q, n_select, sinks=1, recent=1, lens=None, seq=None, max_len=None, **kw):
         """Attention of row r over the n_select pages of sequence r that its query
-        selects (`update_bounds` has to have seen its tokens)."""
+        selects (`update_bounds` has to have seen its tokens); with seq [rows] over
+        those of sequence seq[r], whose first lens[r] keys it sees.  `max_len` bounds
+        the lengths: the tighter, the fewer pages are looked at."""
         if self.bounds is None:
             _refuse("the cache keeps no bounds (bounds=True)")
-        columns = select_pages(q, self.bounds[layer], self.table, self.lens, self.page_size, n_select, sinks=sinks, recent=recent)
-        return sparse_attention(q, self.k[layer], self.v[layer], self.table, self.lens, columns, **kw)
+        lens = self._row_lens(lens, seq)
+        columns = select_pages(q, self.bounds[layer], self.table, lens, self.page_size, n_select, sinks=sinks, recent=recent,
+                               seq=seq, max_len=max_len)
+        return sparse_attention(q, self.k[layer], self.v[layer], self.table, lens, columns, seq=seq, **kw)
 
-    def weigh(self, layer, q, weight, **kw):
-        """Attention of row r over sequence r that adds its weights to `weight`."""
-        return weigh(q, self.k[layer], self.v[layer], self.table, self.lens, weight, **kw)
+    def weigh(self, layer, q, weight, lens=None, seq=None, **kw):
+        """Attention of row r over sequence r that adds its weights to weight[r];
+        with seq [rows] over the first lens[r] keys of sequence seq[r]."""
+        lens = self._row_lens(lens, seq)
+        return weigh(q, self.k[layer], self.v[layer], self.table, lens, weight, seq=seq, **kw)
 
     def evict(self, weight, budget, sinks=0, recent=1):
         """Cuts every sequence to its `budget` heaviest keys (see `evict`), in place,

@@ -26,3 +26,12 @@ def test_evict_refuses_weights_that_it_could_not_cut_in_place(view):
     assert weight.shape == (LAYERS, SEQS, KV, PS * WIDTH)
     with pytest.raises(dexlib.DexError, match="contiguous"):
         cache().evict(weight, 4)
+
+
+def test_rows_of_other_sequences_come_with_their_lengths():
+    """cache.lens[r] is sequence r's length, not that of sequence seq[r]."""
+    seq, q = torch.tensor([2, 0, 1], dtype=torch.int32), torch.zeros((SEQS, 4, HD))
+    c = cache(bounds=True)
+    for call in (lambda: c.sparse_attention(0, q, 2, seq=seq), lambda: c.weigh(0, q, torch.zeros((SEQS, KV, PS * WIDTH)), seq=seq)):
+        with pytest.raises(dexlib.DexError, match="lens"):
+            call()
