@@ -717,10 +717,11 @@ def weigh(q, k_pages, v_pages, table, lens, weight, weight_out=None, seq=None, m
 def evict(weight, lens, budget, sinks=0, recent=1, weight_out=None):
     """Which keys of each sequence and kv head stay, by their accumulated weight
     [n_seqs, n_kv_heads, n] float32: the first `sinks`, the last `recent` and the
-    heaviest others, min(lens[s], budget) in all.  Returns index [n_seqs,
-    n_kv_heads, budget] int32, ascending, then -1, as `keep` takes it, and count
-    [n_seqs], the sequences' new lengths; weight_out (`weight` without it)
-    receives the kept keys' weights, then 0."""
+    heaviest others, min(lens[s], n, budget) in all (keys from n on, which have no
+    weight, do not stay).  Returns index [n_seqs, n_kv_heads, budget] int32,
+    ascending, then -1, as `keep` takes it, and count [n_seqs], the sequences' new
+    lengths; weight_out (`weight` without it) receives the kept keys' weights,
+    then 0."""
     _detached(weight, weight_out)
     if weight.device.type != "cuda":
         _refuse("weight is not on a GPU")
@@ -846,15 +847,19 @@ class PagedCache:
         lens = self._row_lens(lens, seq)
         return weigh(q, self.k[layer], self.v[layer], self.table, lens, weight, seq=seq, **kw)
 
-    def evict(self, weight, budget, sinks=0, recent=1):
+    def evict(self, weight, budget, sinks=0, recent=1, max_len=None):
         """Cuts every sequence to its `budget` heaviest keys (see `evict`), in place,
-        by weight [n_layers, n_seqs, n_kv_heads, n], which is cut with it.  The
-        sequences' pages have no other holders.  The keys keep the rotary positions
-        that they have, and new tokens need positions of the caller's own count."""
+        by weight [n_layers, n_seqs, n_kv_heads, n], which is cut with it; n is at
+        least max_len, which bounds the sequences' lengths (the table's width
+        without it).  The sequences' pages have no other holders.  The keys keep the
+        rotary positions that they have, and new tokens need positions of the
+        caller's own count."""
         if weight.dim() != 4 or weight.shape[:3] != (self.n_layers, len(self.lens), self.k.shape[2]):
             _refuse("weight is [n_layers, n_seqs, n_kv_heads, n]")
         if not weight.is_contiguous():            # (flattened it would be a copy, and only that be cut)
             _refuse("weight is not contiguous")
+        if weight.shape[3] < _max_len(max_len, self.table.shape[1] * self.page_size):
+            _refuse("the weights have fewer columns than max_len")
         self._check_copy()
         n = len(self.lens)
         index, count = evict(weight.flatten(0, 1), self.lens.repeat(self.n_layers), budget, sinks=sinks, recent=recent)

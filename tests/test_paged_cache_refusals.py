@@ -35,3 +35,16 @@ def test_rows_of_other_sequences_come_with_their_lengths():
     for call in (lambda: c.sparse_attention(0, q, 2, seq=seq), lambda: c.weigh(0, q, torch.zeros((SEQS, KV, PS * WIDTH)), seq=seq)):
         with pytest.raises(dexlib.DexError, match="lens"):
             call()
+
+
+def test_evict_refuses_weights_narrower_than_the_sequences_may_be():
+    """Keys without a weight, the most recent ones, would be dropped."""
+    narrow = torch.zeros((LAYERS, SEQS, KV, PS * WIDTH - 1))
+    for max_len in (None, PS * WIDTH, 1 << 40):
+        with pytest.raises(dexlib.DexError, match="columns"):
+            cache().evict(narrow, 4, max_len=max_len)
+    with pytest.raises(dexlib.DexError, match="max_len"):
+        cache().evict(narrow, 4, max_len=-1)
+    for weight, max_len in ((narrow, PS * WIDTH - 1), (narrow, 3), (torch.zeros((LAYERS, SEQS, KV, PS * WIDTH)), None)):
+        with pytest.raises(dexlib.DexError, match="GPU"):     # wide enough: refused for where it is alone
+            cache().evict(weight, 4, max_len=max_len)
