@@ -818,7 +818,8 @@ class PagedCache:
     def update_bounds(self, layer, n_new=None):
         """The bounds of the pages that hold the last n_new tokens (all without
         it); after `fork`, `reserve` and `append` those of the new tokens, after
-        `compact` or `evict` all."""
+        `accept` those of the accepted ones, which have moved (n_new as many as a
+        path has at most), after `compact` or `evict` all."""
         if self.bounds is None:
             _refuse("the cache keeps no bounds (bounds=True)")
         page_bounds(self.k[layer], self.table, self.lens, n_new=n_new, out=self.bounds[layer])
