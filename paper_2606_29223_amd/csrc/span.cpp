@@ -171,6 +171,7 @@ dex_status dex_pages_weigh(int32_t dtype, int32_t head_dim, int32_t n_heads, int
   REFUSE_IF(!weight || !weight_out, "weight or weight_out is NULL");
   REFUSE_IF(!words(weight, weight_out), kType);
   REFUSE_IF(weight_ld < max_len || weight_out_ld < max_len, "a row of the weights is shorter than max_len");
+  REFUSE_IF(weight == weight_out && weight_ld != weight_out_ld, "weight_out is weight with another stride");
   REFUSE_IF(overlaps(n_rows, out_row, n_heads, out_head, head_dim), kOverlap);
   SpanArgs a = span_args(head_dim, n_heads, n_kv_heads, n_rows, 1, row_seq, row_len, max_len, scale, q, q_row, q_head,
                          k_pages, v_pages, n_pages, page_size, table, n_seqs, max_pages, out, out_row, out_head, lse, work);
