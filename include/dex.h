@@ -553,7 +553,10 @@ dex_status dex_beam_select(int32_t dtype, const void *logits, int64_t ld, int32_
  * and eviction by accumulated attention weight.  What is said above of arrays,
  * streams, work memory and refusals holds here too.  head_dim of the attention
  * calls and of bounds and selection is 32, 64 or 128, n_heads a multiple of
- * n_kv_heads, at most 64 times it and 8192, rows * n_heads <= 2^30.
+ * n_kv_heads, at most 64 times it and 8192, rows * n_heads <= 2^30.  A launch
+ * has fewer than 2^32 threads, and a call that would need more is refused: from
+ * 2^24 pairs of a row or sequence and a kv head on, or from 2^22 where a pair has
+ * 1024 threads or four workgroups.
  * ------------------------------------------------------------------------- */
 
 /* Trees.  Node i < draft (1 to 256) of tree b is a drafted token, parent[b][i]

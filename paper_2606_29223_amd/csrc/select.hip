@@ -440,13 +440,48 @@ __global__ __launch_bounds__(TH) void evict_kernel(EvictArgs a) {
 
 int columns_of(int page_shift, int max_len) { return (int)(((int64_t)max_len + (1 << page_shift) - 1) >> page_shift); }
 
+// The (page, kv head) pairs of a sequence, and the workgroups of all.
+struct BoundsGrid {
+  int64_t items, blocks;
+};
+BoundsGrid bounds_grid(const BoundsArgs &a) {
+  const int64_t pages = (((int64_t)a.n_new + (1 << a.map.shift) - 2) >> a.map.shift) + 1, items = pages * a.map.n_kv_heads;
+  return {items, (items * a.map.n_seqs + THREADS / 64 - 1) / (THREADS / 64)};
+}
+
+// The workgroups that score a (row, kv head)'s columns, and the threads that
+// choose among them: as many as keep all in registers, which few threads pass
+// faster: 8 rows of 500 14 us with 256, 18 with 1024, of 6000 24 and 20.
+struct SelectGrid {
+  int columns, parts, threads;
+  int64_t heads;
+};
+SelectGrid select_grid(int dtype, const SelectArgs &a) {
+  const int chunk = 16 / (dtype == DEX_F32 ? 4 : 2), per = THREADS / (a.head_dim / chunk) * SCORE_EACH;
+  const int columns = columns_of(a.map.shift, a.max_len);
+  return {columns, (columns + per - 1) / per, columns <= 2048 ? 256 : 1024, (int64_t)a.n_rows * a.map.n_kv_heads};
+}
+
+// As many threads and keys a thread as keep them all in registers: 256 rows of 700
+// 7.7 us so, 12 and 17 in the wider two; 8 of 4100 15.4, 18.7 in the narrow one
+// and 18.8 in the widest; 32 of 16000 36, 55 and 42 in the others.
+int evict_threads(int capacity) { return capacity <= 1024 ? 256 : 1024; }
+
 }  // namespace
 
+bool bounds_fits(const BoundsArgs &a) {
+  const BoundsGrid g = bounds_grid(a);
+  return g.items <= 0x7fffffff && launch_fits(g.blocks, THREADS);
+}
+bool select_fits(int dtype, const SelectArgs &a) {
+  const SelectGrid g = select_grid(dtype, a);
+  return launch_fits(g.heads * g.parts, THREADS) && launch_fits(g.heads, g.threads);
+}
+bool evict_fits(const EvictArgs &a) { return launch_fits((int64_t)a.n * a.heads, evict_threads(a.capacity)); }
+
 hipError_t launch_bounds(int dtype, const BoundsArgs &a, hipStream_t s) {
-  const int64_t pages = (((int64_t)a.n_new + (1 << a.map.shift) - 2) >> a.map.shift) + 1;
-  const int64_t items = pages * a.map.n_kv_heads, grid = (items * a.map.n_seqs + THREADS / 64 - 1) / (THREADS / 64);
-  if (items > 0x7fffffff || grid > 0x7fffffff) return hipErrorInvalidValue;
-#define DEX_BOUNDS(T, HD) bounds_kernel<T, HD><<<(unsigned)grid, THREADS, 0, s>>>(a, (int)items)
+  const BoundsGrid g = bounds_grid(a);
+#define DEX_BOUNDS(T, HD) bounds_kernel<T, HD><<<(unsigned)g.blocks, THREADS, 0, s>>>(a, (int)g.items)
   if (dtype == DEX_F32) {
     if (a.head_dim == 32) DEX_BOUNDS(float, 32);
     else if (a.head_dim == 64) DEX_BOUNDS(float, 64);
@@ -465,15 +500,11 @@ size_t select_work(int n_rows, int n_kv_heads, int page_shift, int max_len) {
 }
 
 hipError_t launch_select(int dtype, const SelectArgs &a, hipStream_t s) {
-  const int columns = columns_of(a.map.shift, a.max_len), heads = a.n_rows * a.map.n_kv_heads;
-  if (columns > 0) {
-    const int chunk = 16 / (dtype == DEX_F32 ? 4 : 2), per = THREADS / (a.head_dim / chunk) * SCORE_EACH;
-    const int parts = (columns + per - 1) / per;
-    const int64_t grid = (int64_t)parts * heads;
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  const SelectGrid g = select_grid(dtype, a);
+  if (g.columns > 0) {
     const int64_t elem = dtype == DEX_F32 ? 4 : 2;
     const bool whole = (uintptr_t)a.q % 16 == 0 && a.q_row * elem % 16 == 0 && a.q_head * elem % 16 == 0;
-#define DEX_SCORE(T, HD) score_kernel<T, HD><<<(unsigned)grid, THREADS, 0, s>>>(a, columns, parts, whole)
+#define DEX_SCORE(T, HD) score_kernel<T, HD><<<(unsigned)(g.heads * g.parts), THREADS, 0, s>>>(a, g.columns, g.parts, whole)
     if (dtype == DEX_F32) {
       if (a.head_dim == 32) DEX_SCORE(float, 32);
       else if (a.head_dim == 64) DEX_SCORE(float, 64);
@@ -487,19 +518,14 @@ hipError_t launch_select(int dtype, const SelectArgs &a, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  // as many threads as keep all columns in registers, which few threads pass faster:
-  // 8 rows of 500 14 us with 256, 18 with 1024, of 6000 24 and 20
-  if (columns <= 2048) select_kernel<256, 8><<<heads, 256, 0, s>>>(a, columns);
-  else select_kernel<1024, 8><<<heads, 1024, 0, s>>>(a, columns);
+  if (g.threads == 256) select_kernel<256, 8><<<(unsigned)g.heads, 256, 0, s>>>(a, g.columns);
+  else select_kernel<1024, 8><<<(unsigned)g.heads, 1024, 0, s>>>(a, g.columns);
   return hipGetLastError();
 }
 
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s) {
   const int rows = a.n * a.heads;
-  // as many threads and keys a thread as keep them all in registers: 256 rows of 700
-  // 7.7 us so, 12 and 17 in the wider two; 8 of 4100 15.4, 18.7 in the narrow one
-  // and 18.8 in the widest; 32 of 16000 36, 55 and 42 in the others
-  if (a.capacity <= 1024) evict_kernel<256, 4><<<rows, 256, 0, s>>>(a);
+  if (evict_threads(a.capacity) == 256) evict_kernel<256, 4><<<rows, 256, 0, s>>>(a);
   else if (a.capacity <= 8192) evict_kernel<1024, 8><<<rows, 1024, 0, s>>>(a);
   else evict_kernel<1024, 16><<<rows, 1024, 0, s>>>(a);
   return hipGetLastError();

@@ -52,6 +52,16 @@ bool known_sizes(int dtype, int n, int n_heads, int n_kv_heads, int head_dim) {
 const char kWork[] = "the work memory is NULL or not 16-byte aligned";
 const char kDraft[] = "draft is not 1 to 256";
 const char kTrees[] = "n_trees is not 0 to 2^20";
+const char kThreads[] = "a launch would have 2^32 threads or more: too many rows, trees or sequences for one call";
+
+// The limits of weigh and select, keys and pages of all rows and kv heads (max_len at
+// most 2^30).
+bool too_many_keys(int n_rows, int n_kv_heads, int max_len) {
+  return (int64_t)n_rows * n_kv_heads * (max_len / 256 + 1) > (1ll << 30);
+}
+bool too_many_pages(int n_rows, int n_kv_heads, int max_len, int page_size) {
+  return (int64_t)n_rows * n_kv_heads * (max_len / page_size + 128) > (1ll << 33);
+}
 
 }  // namespace
 
@@ -110,6 +120,7 @@ dex_status dex_pages_tree_attention(int32_t dtype, int32_t head_dim, int32_t n_h
   SpanArgs a = span_args(head_dim, n_heads, n_kv_heads, n_trees, draft, tree_seq, tree_len, max_len, scale, q, q_row, q_head,
                          k_pages, v_pages, n_pages, page_size, table, n_seqs, max_pages, out, out_row, out_head, lse, work);
   a.mask = mask; a.words = words_of(draft); a.n_draft = tree_draft;
+  REFUSE_IF(!span_fits(dtype, a), kThreads);
   REFUSE_IF(span_work(dtype, n_trees, draft, n_heads, n_kv_heads, head_dim, max_len, true, false) > 0 &&
                 (!work || !aligned(work, 16)), kWork);
   return launched(fn, launch_span(dtype, a, (hipStream_t)stream));
@@ -143,6 +154,7 @@ dex_status dex_pages_sparse_attention(int32_t dtype, int32_t head_dim, int32_t n
   SpanArgs a = span_args(head_dim, n_heads, n_kv_heads, n_rows, 1, row_seq, row_len, 1 << 30, scale, q, q_row, q_head, k_pages,
                          v_pages, n_pages, page_size, table, n_seqs, max_pages, out, out_row, out_head, lse, work);
   a.columns = columns; a.n_cols = n_columns; a.most = n_columns * page_size;
+  REFUSE_IF(!span_fits(dtype, a), kThreads);
   REFUSE_IF(span_work(dtype, n_rows, 1, n_heads, n_kv_heads, head_dim, a.most, false, false) > 0 &&
                 (!work || !aligned(work, 16)), kWork);
   return launched(fn, launch_span(dtype, a, (hipStream_t)stream));
@@ -150,7 +162,9 @@ dex_status dex_pages_sparse_attention(int32_t dtype, int32_t head_dim, int32_t n
 
 int64_t dex_pages_weigh_work(int32_t dtype, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                              int32_t max_len) {
-  if (!known_sizes(dtype, n_rows, n_heads, n_kv_heads, head_dim) || max_len < 0) return 0;
+  if (!known_sizes(dtype, n_rows, n_heads, n_kv_heads, head_dim) || max_len < 0 || max_len > (1 << 30) ||
+      too_many_keys(n_rows, n_kv_heads, max_len) || (int64_t)n_rows * n_heads > (1 << 30))
+    return 0;
   return (int64_t)span_work(dtype, n_rows, 1, n_heads, n_kv_heads, head_dim, max_len, false, true);
 }
 
@@ -165,7 +179,7 @@ dex_status dex_pages_weigh(int32_t dtype, int32_t head_dim, int32_t n_heads, int
                                         max_pages))
     return refuse(fn, why);
   REFUSE_IF(max_len < 0 || max_len > (1 << 30), "max_len is not 0 to 2^30");
-  REFUSE_IF((int64_t)n_rows * n_kv_heads * (max_len / 256 + 1) > (1ll << 30), "too many keys for one call");
+  REFUSE_IF(too_many_keys(n_rows, n_kv_heads, max_len), "too many keys for one call");
   if (n_rows == 0) return DEX_OK;
   if (const char *why = attention_arrays(dtype, q, k_pages, v_pages, table, row_len, out, row_seq, lse)) return refuse(fn, why);
   REFUSE_IF(!weight || !weight_out, "weight or weight_out is NULL");
@@ -176,6 +190,7 @@ dex_status dex_pages_weigh(int32_t dtype, int32_t head_dim, int32_t n_heads, int
   SpanArgs a = span_args(head_dim, n_heads, n_kv_heads, n_rows, 1, row_seq, row_len, max_len, scale, q, q_row, q_head,
                          k_pages, v_pages, n_pages, page_size, table, n_seqs, max_pages, out, out_row, out_head, lse, work);
   a.weight = weight; a.weight_ld = weight_ld; a.weight_out = weight_out; a.weight_out_ld = weight_out_ld;
+  REFUSE_IF(!span_fits(dtype, a), kThreads);
   REFUSE_IF(!work || !aligned(work, 16), kWork);
   return launched(fn, launch_span(dtype, a, (hipStream_t)stream));
 }
@@ -204,6 +219,7 @@ dex_status dex_pages_keep(int32_t dtype, int32_t head_dim, int32_t n_layers, int
   a.map = PageMap{table, n_seqs, max_pages, n_pages, n_kv_heads, page_shift(page_size)};
   a.to = to_table; a.to_pages = to_pages; a.first = first; a.index = index; a.index_layer = index_layer;
   a.index_seq = index_seq; a.index_head = index_head; a.capacity = capacity; a.count = count;
+  REFUSE_IF(!keep_fits(a), kThreads);
   return launched(fn, launch_keep(a, (hipStream_t)stream));
 }
 
@@ -238,11 +254,13 @@ dex_status dex_pages_bounds(int32_t dtype, int32_t head_dim, const void *k_pages
   BoundsArgs a{};
   a.k = k_pages; a.map = PageMap{table, n_seqs, max_pages, n_pages, n_kv_heads, page_shift(page_size)};
   a.len = length; a.head_dim = head_dim; a.n_new = n_new; a.bounds = bounds;
+  REFUSE_IF(!bounds_fits(a), kThreads);
   return launched(fn, launch_bounds(dtype, a, (hipStream_t)stream));
 }
 
 int64_t dex_pages_select_work(int32_t n_rows, int32_t n_kv_heads, int32_t page_size, int32_t max_len) {
-  if (n_rows < 0 || n_rows > (1 << 20) || n_kv_heads < 1 || n_kv_heads > 4096 || page_shift(page_size) < 0 || max_len < 0)
+  if (n_rows < 0 || n_rows > (1 << 20) || n_kv_heads < 1 || n_kv_heads > 4096 || page_shift(page_size) < 0 || max_len < 0 ||
+      max_len > (1 << 30) || too_many_pages(n_rows, n_kv_heads, max_len, page_size))
     return 0;
   return (int64_t)select_work(n_rows, n_kv_heads, page_shift(page_size), max_len);
 }
@@ -259,7 +277,7 @@ dex_status dex_pages_select(int32_t dtype, int32_t head_dim, int32_t n_heads, in
   REFUSE_IF(max_len < 0 || max_len > (1 << 30), "max_len is not 0 to 2^30");
   REFUSE_IF(sinks < 0 || recent < 0 || sinks > (1 << 30) || recent > (1 << 30), "sinks or recent is not 0 to 2^30");
   REFUSE_IF(n_select < 1 || n_select > (1 << 30) || n_select < (int64_t)sinks + recent, "n_select is below 1 or sinks + recent");
-  REFUSE_IF((int64_t)n_rows * n_kv_heads * (max_len / page_size + 128) > (1ll << 33), "too many pages for one call");
+  REFUSE_IF(too_many_pages(n_rows, n_kv_heads, max_len, page_size), "too many pages for one call");
   if (n_rows == 0) return DEX_OK;
   REFUSE_IF(!q || !bounds || !table || !row_len || !columns, "queries, bounds, table, lengths or columns are NULL");
   REFUSE_IF(!aligned(bounds, 16), "the bounds are not 16-byte aligned");
@@ -270,6 +288,7 @@ dex_status dex_pages_select(int32_t dtype, int32_t head_dim, int32_t n_heads, in
   a.map = PageMap{table, n_seqs, max_pages, n_pages, n_kv_heads, page_shift(page_size)};
   a.seq = row_seq; a.len = row_len; a.n_rows = n_rows; a.n_heads = n_heads; a.head_dim = head_dim; a.max_len = max_len;
   a.n_select = n_select; a.sinks = sinks; a.recent = recent; a.columns = columns; a.work = work;
+  REFUSE_IF(!select_fits(dtype, a), kThreads);
   return launched(fn, launch_select(dtype, a, (hipStream_t)stream));
 }
 
@@ -292,6 +311,7 @@ dex_status dex_pages_evict(const float *weight, int64_t weight_ld, int32_t n_seq
   a.weight = weight; a.weight_out = weight_out; a.weight_ld = weight_ld; a.weight_out_ld = weight_out_ld;
   a.capacity = capacity; a.len = length; a.n = n_seqs; a.heads = n_kv_heads; a.budget = budget; a.sinks = sinks;
   a.recent = recent; a.index = index; a.count = count;
+  REFUSE_IF(!evict_fits(a), kThreads);
   return launched(fn, launch_evict(a, (hipStream_t)stream));
 }
 

@@ -8,6 +8,10 @@ namespace dex {
 
 constexpr int kMaxDraft = 256;          // drafted tokens of a tree
 
+// A launch has fewer than 2^32 threads in a dimension.  Whether the launches of
+// a call have (*_fits) is asked before the first of them.
+inline bool launch_fits(int64_t blocks, int threads) { return blocks <= (int64_t)0xffffffff / threads; }
+
 // Attention of `draft` rows a sequence over its keys (span_attn.hip).
 struct SpanArgs {
   const void *q;
@@ -36,6 +40,7 @@ struct SpanArgs {
   void *work;
 };
 size_t span_work(int dtype, int n, int draft, int n_heads, int n_kv_heads, int head_dim, int most, bool trees, bool weigh);
+bool span_fits(int dtype, const SpanArgs &a);
 hipError_t launch_span(int dtype, const SpanArgs &a, hipStream_t s);
 
 struct TreeMaskArgs {
@@ -67,6 +72,7 @@ struct KeepArgs {
   int capacity;
   const int *count;                     // [n_seqs]
 };
+bool keep_fits(const KeepArgs &a);
 hipError_t launch_keep(const KeepArgs &a, hipStream_t s);
 
 struct TrimArgs {
@@ -83,6 +89,7 @@ struct BoundsArgs {
   int head_dim, n_new;
   void *bounds;                         // [n_pages][n_kv_heads][2][head_dim]
 };
+bool bounds_fits(const BoundsArgs &a);
 hipError_t launch_bounds(int dtype, const BoundsArgs &a, hipStream_t s);
 
 struct SelectArgs {
@@ -97,6 +104,7 @@ struct SelectArgs {
   void *work;
 };
 size_t select_work(int n_rows, int n_kv_heads, int page_shift, int max_len);
+bool select_fits(int dtype, const SelectArgs &a);
 hipError_t launch_select(int dtype, const SelectArgs &a, hipStream_t s);
 
 struct EvictArgs {
@@ -109,6 +117,7 @@ struct EvictArgs {
   int *index;                           // [n][heads][budget]
   int *count;                           // [n]
 };
+bool evict_fits(const EvictArgs &a);
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s);
 
 }  // namespace dex

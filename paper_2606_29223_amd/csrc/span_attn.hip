@@ -878,6 +878,8 @@ struct SpanSizes {
   int blocks, smax, least, step;
   size_t records, stats, scores;          // bytes
   int64_t score_ld;
+  int64_t grid, join, parts, weights;     // workgroups of the kernels (0: not launched); of a row's weights
+  bool fits;
 };
 template <typename T, int HD, int NB, int WC>
 SpanSizes sizes_of(int n, int draft, int n_heads, int n_kv_heads, int keys, bool trees, bool weigh) {
@@ -903,6 +905,12 @@ SpanSizes sizes_of(int n, int draft, int n_heads, int n_kv_heads, int keys, bool
   z.stats = (z.stats + 15) / 16 * 16;
   z.score_ld = weigh ? (most + S::STEP - 1) / S::STEP * S::STEP : 0;
   z.scores = weigh ? (size_t)n * n_heads * z.score_ld * sizeof(float) : 0;
+  constexpr int PER = 256 / (HD / 4);
+  z.grid = items * z.smax;
+  z.join = z.smax > 1 ? ((int64_t)heads + PER - 1) / PER : 0;
+  z.parts = weigh ? (most + WEIGH_KEYS - 1) / WEIGH_KEYS : 0;
+  z.weights = z.parts * n * n_kv_heads;
+  z.fits = launch_fits(z.grid, 64 * S::NW) && launch_fits(z.join, 256) && launch_fits(z.weights, 256);
   return z;
 }
 
@@ -923,22 +931,16 @@ hipError_t go(const SpanArgs &a, hipStream_t s) {
     return (uintptr_t)p % 16 == 0 && row * sizeof(T) % 16 == 0 && head * sizeof(T) % 16 == 0;
   };
   g.whole = whole(a.q, a.q_row, a.q_head) && whole(a.out, a.out_row, a.out_head);
-  const int64_t grid = (int64_t)a.n * a.map.n_kv_heads * z.blocks * z.smax;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  span_attn_kernel<TREE, T, HD, NB, WC><<<(unsigned)grid, 64 * S::NW, 0, s>>>(a, g);
+  span_attn_kernel<TREE, T, HD, NB, WC><<<(unsigned)z.grid, 64 * S::NW, 0, s>>>(a, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (z.smax > 1) {
-    constexpr int PER = 256 / (HD / 4);
-    const int64_t heads = (int64_t)a.n * a.draft * a.n_heads;
-    span_join_kernel<T, HD><<<(unsigned)((heads + PER - 1) / PER), 256, 0, s>>>(a, g, z.step);
+  if (z.join > 0) {
+    span_join_kernel<T, HD><<<(unsigned)z.join, 256, 0, s>>>(a, g, z.step);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (weigh && a.max_len > 0) {
-    const int64_t parts = ((int64_t)a.max_len + WEIGH_KEYS - 1) / WEIGH_KEYS, blocks = parts * a.n * a.map.n_kv_heads;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    span_weigh_kernel<<<(unsigned)blocks, 256, 0, s>>>(a, g, z.step, (int)parts);
+  if (z.weights > 0) {
+    span_weigh_kernel<<<(unsigned)z.weights, 256, 0, s>>>(a, g, z.step, (int)z.parts);
     e = hipGetLastError();
   }
   return e;
@@ -971,13 +973,24 @@ auto by_type(int dtype, int head_dim, F f) {
 
 }  // namespace
 
-size_t span_work(int dtype, int n, int draft, int n_heads, int n_kv_heads, int head_dim, int most, bool trees, bool weigh) {
+namespace {
+SpanSizes span_sizes(int dtype, int n, int draft, int n_heads, int n_kv_heads, int head_dim, int most, bool trees, bool weigh) {
   return by_type(dtype, head_dim, [&](auto t, auto hd) {
     return by_columns(draft * (n_heads / n_kv_heads), (int64_t)n * n_kv_heads, [&](auto nb, auto wc) {
-      const SpanSizes z = sizes_of<decltype(t), hd.value, nb.value, wc.value>(n, draft, n_heads, n_kv_heads, most, trees, weigh);
-      return z.records + z.stats + z.scores;
+      return sizes_of<decltype(t), hd.value, nb.value, wc.value>(n, draft, n_heads, n_kv_heads, most, trees, weigh);
     });
   });
+}
+}  // namespace
+
+size_t span_work(int dtype, int n, int draft, int n_heads, int n_kv_heads, int head_dim, int most, bool trees, bool weigh) {
+  const SpanSizes z = span_sizes(dtype, n, draft, n_heads, n_kv_heads, head_dim, most, trees, weigh);
+  return z.records + z.stats + z.scores;
+}
+
+bool span_fits(int dtype, const SpanArgs &a) {
+  return span_sizes(dtype, a.n, a.draft, a.n_heads, a.map.n_kv_heads, a.head_dim, a.most, a.mask != nullptr,
+                    a.weight_out != nullptr).fits;
 }
 
 hipError_t launch_span(int dtype, const SpanArgs &a, hipStream_t s) {

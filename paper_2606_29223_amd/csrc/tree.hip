@@ -175,7 +175,43 @@ __global__ __launch_bounds__(256) void trim_kernel(TrimArgs a) {
   for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < entries; e += (int64_t)gridDim.x * 256) trim_entry(a, e);
 }
 
+// How a call's lists are cut.  Short lists (a tree's path) take several pairs a
+// workgroup, as long as there are 512 workgroups: 4 lists of 200 in 8 heads 67 us
+// with eight pairs, 10 with one.  Long ones in place go in turns of as much as
+// 1024 threads hold, in slices of 128 bytes, or of 64 where those are fewer than
+// 256 workgroups: 128 lists of 2000 of bf16 rows of 128 53 us (4.9 TB/s; 76 with
+// the narrow ones), 16 of 4000 32 (51 with the wide ones).  What does not wait for
+// itself has few loads a thread and many workgroups: 192 lists of up to 1999 fp32
+// rows of 64 into new pages 70 us with two of 16 bytes, 79 with eight.
+struct KeepGrid {
+  bool turn;
+  int lanes, slices, pairs, split, turns;
+  int64_t groups, blocks;
+};
+KeepGrid keep_grid(const KeepArgs &a) {
+  KeepGrid g;
+  const int chunks = a.row_bytes / 16;
+  const int64_t all = (int64_t)a.n_layers * a.map.n_kv_heads, rows = all * a.map.n_seqs;
+  const bool in_place = a.to == nullptr, brief = a.capacity <= 256;
+  g.turn = in_place && !brief;
+  const int wide = std::min(chunks, 8), narrow = std::min(chunks, 4);
+  g.lanes = !g.turn ? chunks : rows * ((chunks + wide - 1) / wide) >= 256 ? wide : narrow;
+  g.slices = (chunks + g.lanes - 1) / g.lanes;
+  g.pairs = brief ? (int)std::max<int64_t>(1, std::min<int64_t>(8, rows / 512)) : 1;
+  g.groups = (all + g.pairs - 1) / g.pairs;
+  g.blocks = (int64_t)a.map.n_seqs * g.groups * g.slices;
+  const int per = (g.turn ? 1024 * 4 : 512 * 2) / g.lanes, most = (int)(((int64_t)g.pairs * a.capacity + per - 1) / per);
+  g.split = in_place ? 1 : std::min(most, 65535);
+  g.turns = (most + g.split - 1) / g.split;
+  return g;
+}
+
 }  // namespace
+
+bool keep_fits(const KeepArgs &a) {
+  const KeepGrid g = keep_grid(a);
+  return launch_fits(g.blocks, g.turn ? 1024 : 512);
+}
 
 hipError_t launch_tree_mask(const TreeMaskArgs &a, hipStream_t s) {
   tree_mask_kernel<<<a.n, (a.draft + 63) / 64 * 64, 0, s>>>(a);
@@ -188,28 +224,10 @@ hipError_t launch_tree_accept(const TreeAcceptArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_keep(const KeepArgs &a, hipStream_t s) {
-  const int chunks = a.row_bytes / 16;
-  const int64_t all = (int64_t)a.n_layers * a.map.n_kv_heads, rows = all * a.map.n_seqs;
-  // Short lists (a tree's path) take several pairs a workgroup, as long as there
-  // are 512 workgroups: 4 lists of 200 in 8 heads 67 us with eight pairs, 10 with
-  // one.  Long ones in place go in turns of as much as 1024 threads hold, in slices
-  // of 128 bytes, or of 64 where those are fewer than 256 workgroups: 128 lists of
-  // 2000 of bf16 rows of 128 53 us (4.9 TB/s; 76 with the narrow ones), 16 of 4000
-  // 32 (51 with the wide ones).  What does not wait for itself has few loads a
-  // thread and many workgroups: 192 lists of up to 1999 fp32 rows of 64 into new
-  // pages 70 us with two of 16 bytes, 79 with eight.
-  const bool in_place = a.to == nullptr, brief = a.capacity <= 256, turn = in_place && !brief;
-  const int wide = std::min(chunks, 8), narrow = std::min(chunks, 4);
-  const int lanes = !turn ? chunks : rows * ((chunks + wide - 1) / wide) >= 256 ? wide : narrow;
-  const int slices = (chunks + lanes - 1) / lanes;
-  const int pairs = brief ? (int)std::max<int64_t>(1, std::min<int64_t>(8, rows / 512)) : 1;
-  const int64_t groups = (all + pairs - 1) / pairs, blocks = (int64_t)a.map.n_seqs * groups * slices;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  const int per = (turn ? 1024 * 4 : 512 * 2) / lanes, most = (int)(((int64_t)pairs * a.capacity + per - 1) / per);
-  const int split = in_place ? 1 : std::min(most, 65535), turns = (most + split - 1) / split;
-  const dim3 grid((unsigned)blocks, split);
-  if (turn) keep_kernel<1024, 4><<<grid, 1024, 0, s>>>(a, lanes, slices, pairs, (int)groups, turns);
-  else keep_kernel<512, 2><<<grid, 512, 0, s>>>(a, lanes, slices, pairs, (int)groups, turns);
+  const KeepGrid g = keep_grid(a);
+  const dim3 grid((unsigned)g.blocks, g.split);
+  if (g.turn) keep_kernel<1024, 4><<<grid, 1024, 0, s>>>(a, g.lanes, g.slices, g.pairs, (int)g.groups, g.turns);
+  else keep_kernel<512, 2><<<grid, 512, 0, s>>>(a, g.lanes, g.slices, g.pairs, (int)g.groups, g.turns);
   return hipGetLastError();
 }
 
