@@ -589,7 +589,8 @@ dex_status dex_tree_accept(const int32_t *parent, const int32_t *token, const in
  * infinity neither.  Softmax, out and lse as dex_pages_attention's, in all
  * attention below: a weight under 2^-126 of the row's largest may count as 0 (in
  * bf16 as 2^-132), and an infinite value with such a weight gives infinity or
- * NaN.  A row that sees nothing, and the rows from tree_draft[b] on, get zeros
+ * NaN; sums are formed with weights up to 2^8, so values past 2^119 may give
+ * infinity.  A row that sees nothing, and the rows from tree_draft[b] on, get zeros
  * and -inf.                                                                   */
 int64_t dex_pages_tree_attention_work(int32_t dtype, int32_t n_trees, int32_t draft, int32_t n_heads, int32_t n_kv_heads,
                                       int32_t head_dim, int32_t max_len);

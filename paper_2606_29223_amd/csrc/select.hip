@@ -9,10 +9,11 @@
 //
 // On one MI355X: the bounds of 32 rows' last pages 5.0 us and of a whole step's
 // pages a stream over their keys; the scores of 32 ragged rows up to 16000 keys in
-// pages of 32, 8 kv heads of 128, 18 us (20 MB: bounded by the double products and
-// by their conversions, eight waves a SIMD of 2 us each), the choice of 64 of up to 500
-// pages 9.8 us and of 1999 of up to 9000 keys 27 (192 lists), by the latency of the
-// passes: range, one or two digits, places, with barriers between.
+// pages of 32, 8 kv heads of 128, 18 us for 20 MB: 696 of 2048 workgroups have pages,
+// and as a row has eight parts, part p of every row is on one XCD, 256 of the 696
+// on the first and 8 on the last.  The choice of 64 of up to 500 pages 9.8 us and of
+// 1999 of up to 9000 keys 27 (192 lists), by the latency of the passes: range, one or
+// two digits, places, with barriers between.
 #include "dex.h"
 #include "dex_kernels.h"
 #include "span.h"

@@ -12,14 +12,17 @@
 // read for all of them, and a score lies in the lane that needs it as a weight.
 //
 // What bounds it, bf16 heads of 128, 8 kv heads of 4 query heads, on one MI355X:
-// * 8 sequences of 8200 keys, trees of 64 (256 columns): 163 us without the join.
-//   The weights go to the matrix cores in three bf16 parts that hold all 24 bits,
-//   four products a key and column for the two of the formula: 138 GFLOP, 0.85
-//   PFLOP/s for the 1.2 of a large library product here.  A step of a wave has
-//   2048 cycles of products and as much vector work as fits between them (2.4 us
-//   for two waves a SIMD).  Two parts would take 12 % less and round to 17 bits.
-// * 24 ragged trees of 25 up to 12000 keys: 78 us, of which the CUs' mean is 43 and
-//   the rest the difference between them.
+// * 8 sequences of 8200 keys, trees of 64 (256 columns): 163 to 172 us a call with
+//   its join; in a kernel trace 161 in the first three calls and 189 in the middle
+//   of 24, as the clock falls, and the join 15.  The weights go to the matrix cores
+//   in three bf16 parts that hold all 24 bits, four products a key and column for
+//   the two of the formula: 138 GFLOP, 0.73 to 0.86 PFLOP/s for the 1.2 of a large
+//   library product here.  A step of a wave has 2048 cycles of products and as much
+//   vector work as fits between them (2.4 us for two waves a SIMD).  Two parts
+//   would take 12 % less and round to 17 bits.
+// * 24 ragged trees of 25 up to 12000 keys: 79 us, of which the CUs' mean is 43 and
+//   the rest the difference between them.  Columns of rows behind n_draft, half of
+//   all here, are computed like the others.
 // * 32 single rows of 4000 keys: 5.3 TB/s in the kernel, memory's.
 // Not better: tiles of 64 keys (they spill, or are equal), three waves a SIMD
 // (spills), eight waves a workgroup (equal), the ring four tiles deep (181 us for
