@@ -108,9 +108,9 @@ __device__ __forceinline__ float quarters_sum(float v) {
 // make it NaN).  The two add at most 2^-132 to a weight, which goes to 0 below
 // 2^-126 in the power already; only of a weight of 0 would that be too much where
 // the key is hidden, so in steps with drafted keys, where values that are no
-// finite numbers go by themselves, the parts are what they are.  (Of a weight of
-// 0 made 0 in all steps, which is one instruction more for two weights: 8 trees of
-// 64 over 8200 keys 167 us for 164, 24 ragged ones of 25 85 for 81.)
+// finite numbers go by themselves, the parts are what they are.  (To make them 0 for
+// a weight of 0 in all steps is one instruction more for two weights: 8 trees of 64
+// over 8200 keys 167 us for 164, 24 ragged ones of 25 85 for 81.)
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }

@@ -142,3 +142,15 @@ def test_large_values_of_single_rows(dtype, group):
         for bad in (float("inf"), float("-inf")):
             got = run(*_underflow(dtype, keys, at, score, bad))
             assert (got[..., 3] == bad).all() and np.isfinite(np.delete(got, 3, 2)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("score", [0.0, 32.0, -32.0])
+def test_infinite_values_with_weights_of_few_bits(dtype, score):
+    """The row's largest key has weight 1, whose lower parts are nothing, and one
+    value of it is infinite."""
+    torch_cuda()
+    for keys, at in ((40, 3), (900, 500), (900, 899)):
+        for bad in (float("inf"), float("-inf")):
+            for got in _every_form(*_underflow(dtype, keys, at, score, bad), keys):
+                assert (got[..., 3] == bad).all() and np.isfinite(np.delete(got, 3, 2)).all()
